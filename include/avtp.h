@@ -62,7 +62,10 @@ typedef enum {
 #define AVTP_FLAG_NAN_SCORE 1       /* a visual score was NaN (ranked last)           */
 #define AVTP_FLAG_NO_TEXT_AFTER 2   /* an image has no text row after it (scores = 0) */
 #define AVTP_FLAG_INFEASIBLE 4      /* budget bounds cannot meet keep_total           */
-#define AVTP_FLAG_OUT_CAPACITY 8    /* kept list longer than keep_capacity (truncated) */
+#define AVTP_FLAG_OUT_CAPACITY 8    /* kept list longer than keep_capacity (truncated), */
+                                    /* or a full page stack (avtp_page_trim)            */
+#define AVTP_FLAG_BAD_PAGE 16       /* a block table entry in use lies outside the pool */
+#define AVTP_FLAG_NO_PAGES 32       /* avtp_page_tables: a request got no place         */
 
 /* Limits checked on the host (AVTP_ERR_UNSUPPORTED beyond them). */
 #define AVTP_MAX_IMAGES_PER_SEQ 256
@@ -71,6 +74,7 @@ typedef enum {
 #define AVTP_MAX_TENSORS 8
 #define AVTP_MAX_LAYERS 1024       /* avtp_layer_select: layers               */
 #define AVTP_MAX_SAMPLES (1 << 20) /* avtp_layer_select: samples              */
+#define AVTP_MAX_REQUESTS (1 << 16) /* avtp_page_*: sequences of a batch      */
 /* The attention score (avtp_score in attention mode, avtp_row_lse) addresses
  * one sequence's keys and text-row queries with 32-bit byte offsets: every
  * sequence must have (its tokens) * Hkv * d * elem and (its text rows) *
@@ -347,6 +351,121 @@ int avtp_score_noalloc(avtp_stream_t stream, const avtp_layout *layout, int mode
                        float softmax_scale, const float *row_lse, const void *h_cur,
                        const void *h_prior, int hidden, float *scores, float *img_sum,
                        int32_t *status);
+
+/* ------------------------------------------------------------------------
+ * The paged K/V cache.  Pruning leaves every sequence of every layer with a
+ * length of its own (Sec. 3.3.3: the keep count of each image; Sec. 3.3.2: a
+ * progressive schedule shortens the sequence again at each pruning layer), so
+ * a layer's K and V are kept in pages of page_size tokens that sequences take
+ * and hand back one at a time:
+ *   k, v  [n_pages][Hkv][page_size][d] (dtype), page_size a power of two in
+ *         [16, 1024], d in {64, 128}; token t of sequence b lies at place
+ *         t mod page_size of page block_table[b][t / page_size];
+ *   block_table [B][max_pages] int32, in token order;
+ *   free_pages  [n_pages] int32, a stack of page ids: the first free_count[0]
+ *         entries are free, the next page taken is the last of them;
+ *   slot  page * page_size + place, the place of one token (int32, so
+ *         n_pages * page_size is below 2^31).
+ * A model's layers may share one table (same lengths) or have one each.  All
+ * of it lives on the device and no call reads it back, so a step of a serving
+ * loop can be captured into a graph: tables, store, attention, trim.  Updated
+ * lengths and counts go to buffers of their own (outputs must not alias
+ * inputs; only block_table, free_pages and the pages are updated in place).
+ * B is at most AVTP_MAX_REQUESTS, B * max_pages below 2^31.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  void *k, *v;
+  int32_t dtype, n_pages, page_size, Hkv, d;
+} avtp_pages;
+
+/* ------------------------------------------------------------------------
+ * avtp_page_tables -- room for the new tokens of every request: block tables
+ * and slot map from the request lengths.  Sequence b holds seq_len[b] tokens
+ * and gets the next cu_new[b+1] - cu_new[b] ones, whose index in this step's
+ * batch starts at cu_new[b] (cu_new[0] = 0; e.g. cu_out of a selection).  The
+ * pages it lacks are popped off the stack, sequences in order, and entered in
+ * its row of the table; other entries stay as they were.
+ *   slot_map [n_new] int32 (output): the slot of every new token; -1 for
+ *     tokens without a place and for entries from cu_new[B] on (a padded
+ *     batch).
+ *   seq_len_out [B], free_count_out [1] int32 (outputs): the state afterwards.
+ * A request has no place if its row of the table is too short, if its new
+ * tokens reach past n_new, or (needing pages) if the pages it and the requests before it need are more than the
+ * stack holds: its length and row stay as they were, its slots are -1 and it
+ * flags AVTP_FLAG_NO_PAGES.  A page id outside [0, n_pages) gives slots of -1
+ * and flags AVTP_FLAG_BAD_PAGE.  free_count is read as at most n_pages.
+ * ---------------------------------------------------------------------- */
+int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
+                     const int32_t *seq_len, const int32_t *free_pages, int n_pages,
+                     const int32_t *free_count, int32_t *block_table, int max_pages,
+                     int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
+                     int32_t *free_count_out, int32_t *status);
+
+/* ------------------------------------------------------------------------
+ * avtp_page_trim -- sequences are cut to their first keep_len[b] tokens (0: the
+ * request has ended; seq_len[b] or more: nothing changes; less: tokens are
+ * taken back, e.g. rejected drafts).  The pages that hold none of the kept
+ * tokens are pushed onto the stack, sequences in order, each one's in token
+ * order; the table is only read.  seq_len_out [B] = min(keep_len, seq_len),
+ * free_count_out [1].  Pages beyond the stack's n_pages entries (more pages
+ * handed back than the pool has) are dropped and flag AVTP_FLAG_OUT_CAPACITY.
+ * ---------------------------------------------------------------------- */
+int avtp_page_trim(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
+                   const int32_t *seq_len, const int32_t *block_table, int max_pages,
+                   int32_t *free_pages, int n_pages, const int32_t *free_count,
+                   int32_t *seq_len_out, int32_t *free_count_out, int32_t *status);
+
+/* ------------------------------------------------------------------------
+ * avtp_page_store -- K and V rows into their pages: for every r < n with slot
+ * s = slot_map[r], row keep_idx[r] (row r when keep_idx is NULL) of k and v
+ * [n_src, Hkv, d] goes to place s of the pages.  With the keep_idx of a
+ * selection and the slot map of its cu_out this is the compaction of a pruned
+ * layer's K and V (avtp_compact), straight into the cache.  k_stride and
+ * v_stride: elements from one token to the next (Hkv * d or more; slices of a
+ * fused projection are read in place).  Rows and strides are 16-byte aligned.
+ * A slot outside the pool or a keep_idx entry outside [0, n_src) writes
+ * nothing.  Of two rows with one slot either may stay.  Bit-exact.
+ * ---------------------------------------------------------------------- */
+int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k, int64_t k_stride,
+                    const void *v, int64_t v_stride, int64_t n_src, const int32_t *slot_map,
+                    const int32_t *keep_idx, int64_t n);
+
+/* ------------------------------------------------------------------------
+ * avtp_page_attention -- the attention of a chunk of new tokens over the
+ * paged cache, their own K and V included.  The queries of sequence b are rows
+ * cu_q[b] .. cu_q[b+1]-1 of q, its last n_b = cu_q[b+1] - cu_q[b] tokens; row t
+ * of them sees the first kv_len[b] - n_b + t + 1 cached tokens.  With c =
+ * softmax_scale and query head h using key head g = h / (Hq/Hkv):
+ *   lse[h,t] = log sum_j exp(c q_{t,h}.k_{j,g}),
+ *   out[t,h] = sum_j exp(c q_{t,h}.k_{j,g} - lse[h,t]) v_{j,g}
+ * over the tokens j the row sees.  A row that sees none (kv_len[b] < n_b): out 0,
+ * lse -inf.  Values of tokens a row does not see do not reach it, whatever they
+ * are, infinities and NaN included.
+ *   q, out  [N_q, Hq, d] (dtype of the pages), q_stride and out_stride elements
+ *     from one token to the next (Hq * d or more), rows and strides 16-byte
+ *     aligned; rows of out from cu_q[B] on stay as they were;
+ *   lse     [Hq, N_q] fp32, natural log (may be NULL): the row_lse of
+ *     avtp_score for the text rows of the layer;
+ *   max_kv_len: a bound on kv_len, which sizes the launch and the workspace
+ *     only (with a lower one the results are the same, slower).
+ * A single new token per sequence is the decode step.  Products of bf16 run on
+ * the bf16 MFMA with fp32 accumulation, the probabilities rounded to bf16 before
+ * they weigh V (2^-8 of each at most); fp32 runs in fp32.  Sums and
+ * maxima are fp32.  A block table entry outside [0, n_pages) reads nothing: its
+ * tokens count as zeros and flag AVTP_FLAG_BAD_PAGE; so does a kv_len above
+ * max_pages * page_size, of which the tokens in the table remain; a negative
+ * one is 0.  No atomics on results: reruns are bit-identical.
+ * ws: device scratch of avtp_page_attention_workspace_size() bytes (which may
+ * be 0, and is for an invalid argument), 256-byte aligned; no initialisation.
+ * N_q * Hq is below 2^31, Hq at most 256.
+ * ---------------------------------------------------------------------- */
+size_t avtp_page_attention_workspace_size(const avtp_pages *pages, int Hq, int B, int64_t N_q,
+                                          int64_t max_kv_len);
+int avtp_page_attention(avtp_stream_t stream, const avtp_pages *pages, const void *q,
+                        int64_t q_stride, int Hq, int B, int64_t N_q, const int32_t *cu_q,
+                        const int32_t *kv_len, const int32_t *block_table, int max_pages,
+                        int64_t max_kv_len, float softmax_scale, void *out, int64_t out_stride,
+                        float *lse, int32_t *status, void *ws, size_t ws_bytes);
 
 /* Human-readable name of an avtp_status value (static string). */
 const char *avtp_status_string(int status);

@@ -25,6 +25,7 @@ BF16, FP32 = 0, 1
 SCORE_ATTN, SCORE_VARIATION = 0, 1
 BUDGET_PROPORTIONAL, BUDGET_RAW = 0, 1
 FLAG_NAN_SCORE, FLAG_NO_TEXT_AFTER, FLAG_INFEASIBLE, FLAG_OUT_CAPACITY = 1, 2, 4, 8
+FLAG_BAD_PAGE, FLAG_NO_PAGES = 16, 32
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_INFEASIBLE, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4, -5
 NOALLOC_MAX_WORKSPACE = 16 << 20   # AVTP_NOALLOC_MAX_WORKSPACE of include/avtp.h
 
@@ -46,6 +47,11 @@ class _Tensor(ctypes.Structure):
                 ("src_stride", ctypes.c_int64), ("dst_stride", ctypes.c_int64),
                 ("planes", ctypes.c_int32), ("src_plane_stride", ctypes.c_int64),
                 ("dst_plane_stride", ctypes.c_int64)]
+
+
+class _Pages(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page_size", "Hkv", "d")]
 
 
 class AvtpError(RuntimeError):
@@ -85,13 +91,23 @@ def lib() -> ctypes.CDLL:
                                                  ctypes.POINTER(_Tensor), c_int]
         L.avtp_layer_attention.argtypes = [vp, LP, vp, vp]
         L.avtp_layer_select.argtypes = [vp, vp, c_int, c_int, c_int, vp, vp]
+        i64, PP = ctypes.c_int64, ctypes.POINTER(_Pages)
+        L.avtp_page_tables.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, vp, c_int, vp, i64,
+                                       vp, vp, vp]
+        L.avtp_page_trim.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, c_int, vp, vp, vp, vp]
+        L.avtp_page_store.argtypes = [vp, PP, vp, i64, vp, i64, i64, vp, vp, i64]
+        L.avtp_page_attention_workspace_size.argtypes = [PP, c_int, c_int, i64, i64]
+        L.avtp_page_attention_workspace_size.restype = sz
+        L.avtp_page_attention.argtypes = [vp, PP, vp, i64, c_int, c_int, i64, vp, vp, vp, c_int, i64,
+                                          c_float, vp, i64, vp, vp, vp, sz]
         L.avtp_status_string.argtypes = [c_int]
         L.avtp_status_string.restype = ctypes.c_char_p
         L.avtp_version.restype = c_int
         for f in ("avtp_score", "avtp_score_noalloc", "avtp_row_lse", "avtp_budget", "avtp_select",
                   "avtp_compact",
                   "avtp_layer_attention", "avtp_layer_select", "avtp_pruned_layout",
-                  "avtp_select_compact", "avtp_budget_select_compact"):
+                  "avtp_select_compact", "avtp_budget_select_compact", "avtp_page_tables",
+                  "avtp_page_trim", "avtp_page_store", "avtp_page_attention"):
             getattr(L, f).restype = c_int
         _lib = L
     return _lib
@@ -607,3 +623,194 @@ def layer_select(A: torch.Tensor, k: int, rank_sum: Optional[torch.Tensor] = Non
                                    _arg(selected, "selected", max(0, int(k)), torch.int32)),
            "avtp_layer_select")
     return rank_sum[:L], selected[:k]
+
+
+# --------------------------------------------------------------------------- the paged K/V cache
+def _page_arg(t: Optional[torch.Tensor], name: str, numel: int = 0, dtype=torch.int32):
+    """``_arg`` for the calls on pages, which also need their tensors on the
+    current device: the stream they run on is that device's."""
+    if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, the current device is "
+                         f"cuda:{torch.cuda.current_device()}")
+    return _arg(t, name, numel, dtype)
+
+
+def _page_rows(t: torch.Tensor, name: str, heads: int, pages: "Pages"):
+    """Pointer and token stride of rows [N, heads, d] (a slice of a fused
+    projection is fine: only the token stride is free)."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != pages.d:
+        raise ValueError(f"{name}: [N, {heads}, {pages.d}] is needed, got {tuple(t.shape)}")
+    if t.dtype != pages.dtype:
+        raise TypeError(f"{name}: {pages.dtype} is needed, got {t.dtype}")
+    _page_arg(t[:0].reshape(-1), name, 0, None)
+    if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != pages.d)):
+        raise ValueError(f"{name}: the values of a token must be contiguous")
+    stride = t.stride(0) if t.shape[0] > 1 else heads * pages.d
+    if t.shape[0] > 1 and stride < heads * pages.d:
+        raise ValueError(f"{name}: tokens overlap (stride {stride})")
+    if t.shape[0] > 0 and (t.data_ptr() % 16 or stride * t.element_size() % 16):
+        raise ValueError(f"{name}: rows and the token stride must be 16-byte aligned")
+    return ctypes.c_void_p(t.data_ptr()), stride
+
+
+class Pages:
+    """The pages of one layer's cache: k and v [n_pages, Hkv, page_size, d]."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if k.dim() != 4 or k.shape != v.shape or k.dtype != v.dtype:
+            raise ValueError("k and v must both be [n_pages, Hkv, page_size, d] of one dtype")
+        self.k, self.v = k, v
+        self.n_pages, self.Hkv, self.page_size, self.d = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        self.st = _Pages(_page_arg(k, "k", 1, None), _page_arg(v, "v", 1, None), dtype_code(k),
+                         self.n_pages, self.page_size, self.Hkv, self.d)
+
+    @classmethod
+    def empty(cls, n_pages: int, Hkv: int, page_size: int, d: int, dtype=torch.bfloat16,
+              device="cuda") -> "Pages":
+        new = lambda: torch.empty((n_pages, Hkv, page_size, d), dtype=dtype, device=device)  # noqa: E731
+        return cls(new(), new())
+
+    def ref(self):
+        return ctypes.byref(self.st)
+
+
+def _check_table(block_table: torch.Tensor, B: int) -> None:
+    if block_table.dim() != 2 or block_table.shape[0] < B or block_table.shape[1] < 1:
+        raise ValueError(f"block_table must be [{B}, max_pages], got {tuple(block_table.shape)}")
+
+
+def prepare_page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Tensor,
+                        free_pages: torch.Tensor, free_count: torch.Tensor,
+                        block_table: torch.Tensor, slot_map: torch.Tensor, seq_len_out: torch.Tensor,
+                        free_count_out: torch.Tensor, status: Optional[torch.Tensor] = None,
+                        stream=None) -> Prepared:
+    """avtp_page_tables on fixed buffers, as a Prepared call."""
+    B = seq_len.numel()
+    _check_table(block_table, B)
+    args = (_stream(stream), B, int(page_size), _page_arg(cu_new, "cu_new", B + 1),
+            _page_arg(seq_len, "seq_len", 1), _page_arg(free_pages, "free_pages", 1),
+            free_pages.numel(), _page_arg(free_count, "free_count", 1),
+            _page_arg(block_table, "block_table"), block_table.shape[1],
+            _page_arg(slot_map, "slot_map"), slot_map.numel(),
+            _page_arg(seq_len_out, "seq_len_out", B), _page_arg(free_count_out, "free_count_out", 1),
+            _page_arg(status, "status", B))
+    return Prepared(lib().avtp_page_tables, args, "avtp_page_tables",
+                    (cu_new, seq_len, free_pages, free_count, block_table, slot_map, seq_len_out,
+                     free_count_out, status, stream))
+
+
+def page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Tensor, free_pages: torch.Tensor,
+                free_count: torch.Tensor, block_table: torch.Tensor, n_new: int,
+                status: Optional[torch.Tensor] = None, stream=None):
+    """Room for the new tokens of every request (block_table is updated in
+    place).  Returns (slot_map [n_new], seq_len_out, free_count_out)."""
+    new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+    slot_map, seq_len_out, free_count_out = new(n_new), new(seq_len.numel()), new(1)
+    prepare_page_tables(page_size, cu_new, seq_len, free_pages, free_count, block_table, slot_map,
+                        seq_len_out, free_count_out, status, stream)()
+    return slot_map, seq_len_out, free_count_out
+
+
+def prepare_page_trim(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor,
+                      block_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                      seq_len_out: torch.Tensor, free_count_out: torch.Tensor,
+                      status: Optional[torch.Tensor] = None, stream=None) -> Prepared:
+    """avtp_page_trim on fixed buffers, as a Prepared call."""
+    B = seq_len.numel()
+    _check_table(block_table, B)
+    args = (_stream(stream), B, int(page_size), _page_arg(keep_len, "keep_len", B),
+            _page_arg(seq_len, "seq_len", 1), _page_arg(block_table, "block_table"),
+            block_table.shape[1], _page_arg(free_pages, "free_pages", 1), free_pages.numel(),
+            _page_arg(free_count, "free_count", 1), _page_arg(seq_len_out, "seq_len_out", B),
+            _page_arg(free_count_out, "free_count_out", 1), _page_arg(status, "status", B))
+    return Prepared(lib().avtp_page_trim, args, "avtp_page_trim",
+                    (keep_len, seq_len, block_table, free_pages, free_count, seq_len_out,
+                     free_count_out, status, stream))
+
+
+def page_trim(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor, block_table: torch.Tensor,
+              free_pages: torch.Tensor, free_count: torch.Tensor,
+              status: Optional[torch.Tensor] = None, stream=None):
+    """Cut every sequence to its first keep_len tokens and push the pages it no
+    longer needs (free_pages is updated in place).  Returns (seq_len_out,
+    free_count_out)."""
+    new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+    seq_len_out, free_count_out = new(seq_len.numel()), new(1)
+    prepare_page_trim(page_size, keep_len, seq_len, block_table, free_pages, free_count, seq_len_out,
+                      free_count_out, status, stream)()
+    return seq_len_out, free_count_out
+
+
+def prepare_page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor,
+                       keep_idx: Optional[torch.Tensor] = None, stream=None) -> Prepared:
+    """avtp_page_store on fixed buffers, as a Prepared call: one row for each
+    entry of slot_map."""
+    n = slot_map.numel()
+    if k.shape != v.shape:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    if keep_idx is None and k.shape[0] < n:
+        raise ValueError(f"slot_map has {n} entries, k and v {k.shape[0]} rows")
+    kp, ks = _page_rows(k, "k", pages.Hkv, pages)
+    vp, vs = _page_rows(v, "v", pages.Hkv, pages)
+    args = (_stream(stream), pages.ref(), kp, ks, vp, vs, k.shape[0], _page_arg(slot_map, "slot_map"),
+            _page_arg(keep_idx, "keep_idx", n), n)
+    return Prepared(lib().avtp_page_store, args, "avtp_page_store",
+                    (pages, k, v, slot_map, keep_idx, stream))
+
+
+def page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor,
+               keep_idx: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of k and v [N, Hkv, d] (the rows keep_idx names, if given) to their
+    slots in the pages."""
+    prepare_page_store(pages, k, v, slot_map, keep_idx, stream)()
+
+
+def page_attention_workspace_bytes(pages: Pages, Hq: int, B: int, N_q: int, max_kv_len: int) -> int:
+    return int(lib().avtp_page_attention_workspace_size(pages.ref(), Hq, B, N_q, max_kv_len))
+
+
+def prepare_page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,
+                           block_table: torch.Tensor, softmax_scale: float, max_kv_len: int,
+                           out: torch.Tensor, ws: Optional[torch.Tensor],
+                           lse: Optional[torch.Tensor] = None,
+                           status: Optional[torch.Tensor] = None, stream=None) -> Prepared:
+    """avtp_page_attention on fixed buffers, as a Prepared call (ws may be None
+    where no workspace is needed)."""
+    B = kv_len.numel()
+    _check_table(block_table, B)
+    if q.dim() != 3 or q.shape != out.shape:
+        raise ValueError(f"q and out must both be [N_q, Hq, d], got {tuple(q.shape)} and {tuple(out.shape)}")
+    N, Hq, _ = q.shape
+    qp, qs = _page_rows(q, "q", Hq, pages)
+    op, os_ = _page_rows(out, "out", Hq, pages)
+    args = (_stream(stream), pages.ref(), qp, qs, Hq, B, N, _page_arg(cu_q, "cu_q", B + 1),
+            _page_arg(kv_len, "kv_len", 1), _page_arg(block_table, "block_table"),
+            block_table.shape[1], int(max_kv_len), float(softmax_scale), op, os_,
+            _page_arg(lse, "lse", Hq * N, torch.float32), _page_arg(status, "status", B),
+            _page_arg(ws, "ws", 0, torch.uint8), 0 if ws is None else ws.numel())
+    return Prepared(lib().avtp_page_attention, args, "avtp_page_attention",
+                    (pages, q, cu_q, kv_len, block_table, out, lse, status, ws, stream))
+
+
+def page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,
+                   block_table: torch.Tensor, softmax_scale: float, max_kv_len: Optional[int] = None,
+                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                   status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
+                   stream=None):
+    """The attention of the last cu_q[b+1] - cu_q[b] tokens of every sequence
+    over its pages; max_kv_len (the table's length by default) sizes the launch.
+    Returns (out [N_q, Hq, d], lse [Hq, N_q])."""
+    N, Hq, _ = q.shape
+    if max_kv_len is None:
+        max_kv_len = block_table.shape[-1] * pages.page_size
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if lse is None:
+        lse = torch.empty((Hq, N), dtype=torch.float32, device=q.device)
+    if ws is None:
+        ws = alloc_workspace(page_attention_workspace_bytes(pages, Hq, kv_len.numel(), N, max_kv_len),
+                             q.device)
+    prepare_page_attention(pages, q, cu_q, kv_len, block_table, softmax_scale, max_kv_len, out, ws,
+                           lse, status, stream)()
+    return out, lse

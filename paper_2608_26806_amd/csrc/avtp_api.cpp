@@ -110,7 +110,7 @@ using namespace avtp;
 
 extern "C" {
 
-int avtp_version(void) { return (1 << 16) | 0; }
+int avtp_version(void) { return (1 << 16) | 1; }
 
 const char *avtp_status_string(int s) {
   switch (s) {
@@ -425,6 +425,125 @@ int avtp_budget_select_compact(avtp_stream_t stream, const avtp_layout *layout,
                                                  hi_permille, floor_abs, scores, budget, keep_idx,
                                                  keep_capacity, cu_out, status, need, tensors,
                                                  n_tensors));
+}
+
+// ---- the paged cache
+
+static bool page_size_ok(int ps) { return ps >= 16 && ps <= 1024 && (ps & (ps - 1)) == 0; }
+
+// sizes shared by the calls on block tables
+static int check_tables(int B, int page_size, int max_pages, int n_pages) {
+  if (B < 1 || max_pages < 1 || n_pages < 1 || page_size < 1) return AVTP_ERR_INVALID_ARG;
+  if (B > AVTP_MAX_REQUESTS || !page_size_ok(page_size)) return AVTP_ERR_UNSUPPORTED;
+  if ((int64_t)B * max_pages > INT32_MAX || (int64_t)max_pages * page_size > INT32_MAX ||
+      (int64_t)n_pages * page_size > INT32_MAX)
+    return AVTP_ERR_UNSUPPORTED;
+  return AVTP_OK;
+}
+
+int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
+                     const int32_t *seq_len, const int32_t *free_pages, int n_pages,
+                     const int32_t *free_count, int32_t *block_table, int max_pages,
+                     int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
+                     int32_t *free_count_out, int32_t *status) {
+  int rc = check_tables(B, page_size, max_pages, n_pages);
+  if (rc != AVTP_OK) return rc;
+  if (!cu_new || !seq_len || !free_pages || !free_count || !block_table || !seq_len_out ||
+      !free_count_out || n_new < 0 || (n_new > 0 && !slot_map))
+    return AVTP_ERR_INVALID_ARG;
+  // blocks read the state that another block would overwrite
+  if (seq_len_out == seq_len || free_count_out == free_count) return AVTP_ERR_INVALID_ARG;
+  if (n_new > INT32_MAX) return AVTP_ERR_UNSUPPORTED;
+  const PageTables P{B,       __builtin_ctz((unsigned)page_size), max_pages,      n_pages, seq_len,
+                     free_count, seq_len_out,                     free_count_out, status};
+  return hip_status(launch_page_tables((hipStream_t)stream, P, cu_new, free_pages, block_table,
+                                       slot_map, n_new));
+}
+
+int avtp_page_trim(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
+                   const int32_t *seq_len, const int32_t *block_table, int max_pages,
+                   int32_t *free_pages, int n_pages, const int32_t *free_count,
+                   int32_t *seq_len_out, int32_t *free_count_out, int32_t *status) {
+  int rc = check_tables(B, page_size, max_pages, n_pages);
+  if (rc != AVTP_OK) return rc;
+  if (!keep_len || !seq_len || !block_table || !free_pages || !free_count || !seq_len_out ||
+      !free_count_out)
+    return AVTP_ERR_INVALID_ARG;
+  if (seq_len_out == seq_len || seq_len_out == keep_len || free_count_out == free_count)
+    return AVTP_ERR_INVALID_ARG;
+  const PageTables P{B,       __builtin_ctz((unsigned)page_size), max_pages,      n_pages, seq_len,
+                     free_count, seq_len_out,                     free_count_out, status};
+  return hip_status(launch_page_trim((hipStream_t)stream, P, keep_len, block_table, free_pages));
+}
+
+// the pool: types, sizes, alignment
+static int check_pages(const avtp_pages *p) {
+  if (!p || !p->k || !p->v || p->n_pages < 1 || p->Hkv < 1 || p->page_size < 1)
+    return AVTP_ERR_INVALID_ARG;
+  if (p->dtype != AVTP_BF16 && p->dtype != AVTP_FP32) return AVTP_ERR_UNSUPPORTED;
+  if ((p->d != 64 && p->d != 128) || p->Hkv > 256 || !page_size_ok(p->page_size))
+    return AVTP_ERR_UNSUPPORTED;
+  if ((int64_t)p->n_pages * p->page_size > INT32_MAX) return AVTP_ERR_UNSUPPORTED;
+  if ((uintptr_t)p->k % 16 || (uintptr_t)p->v % 16) return AVTP_ERR_INVALID_ARG;
+  return AVTP_OK;
+}
+
+// rows of `heads` heads each, `stride` elements apart
+static bool rows_ok(const void *x, int64_t stride, int heads, const avtp_pages &p) {
+  const int64_t es = p.dtype == AVTP_FP32 ? 4 : 2;
+  return x && stride >= (int64_t)heads * p.d && stride <= INT64_MAX / 1024 && stride * es % 16 == 0 &&
+         (uintptr_t)x % 16 == 0;
+}
+
+int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k, int64_t k_stride,
+                    const void *v, int64_t v_stride, int64_t n_src, const int32_t *slot_map,
+                    const int32_t *keep_idx, int64_t n) {
+  int rc = check_pages(pages);
+  if (rc != AVTP_OK) return rc;
+  if (n < 0 || n_src < 0 || (!keep_idx && n > n_src)) return AVTP_ERR_INVALID_ARG;
+  if (n > INT32_MAX || n_src > INT32_MAX) return AVTP_ERR_UNSUPPORTED;
+  if (n == 0 || n_src == 0) return AVTP_OK;
+  if (!slot_map || !rows_ok(k, k_stride, pages->Hkv, *pages) || !rows_ok(v, v_stride, pages->Hkv, *pages))
+    return AVTP_ERR_INVALID_ARG;
+  const int64_t es = pages->dtype == AVTP_FP32 ? 4 : 2;
+  return hip_status(launch_page_store((hipStream_t)stream, *pages, k, k_stride * es, v, v_stride * es,
+                                      n_src, slot_map, keep_idx, n));
+}
+
+static int check_page_attention(const avtp_pages *pages, int Hq, int B, int64_t N_q, int64_t max_kv_len) {
+  int rc = check_pages(pages);
+  if (rc != AVTP_OK) return rc;
+  if ((rc = check_attn_args(pages->dtype, Hq, pages->Hkv, pages->d)) != AVTP_OK) return rc;
+  if (B < 1 || N_q < 0 || max_kv_len < 0) return AVTP_ERR_INVALID_ARG;
+  if (B > AVTP_MAX_REQUESTS || N_q > INT32_MAX / Hq) return AVTP_ERR_UNSUPPORTED;
+  return AVTP_OK;
+}
+
+size_t avtp_page_attention_workspace_size(const avtp_pages *pages, int Hq, int B, int64_t N_q,
+                                          int64_t max_kv_len) {
+  if (check_page_attention(pages, Hq, B, N_q, max_kv_len) != AVTP_OK) return 0;
+  return page_attn_plan(*pages, Hq, B, N_q, max_kv_len).bytes;
+}
+
+int avtp_page_attention(avtp_stream_t stream, const avtp_pages *pages, const void *q,
+                        int64_t q_stride, int Hq, int B, int64_t N_q, const int32_t *cu_q,
+                        const int32_t *kv_len, const int32_t *block_table, int max_pages,
+                        int64_t max_kv_len, float softmax_scale, void *out, int64_t out_stride,
+                        float *lse, int32_t *status, void *ws, size_t ws_bytes) {
+  int rc = check_page_attention(pages, Hq, B, N_q, max_kv_len);
+  if (rc != AVTP_OK) return rc;
+  if ((rc = check_tables(B, pages->page_size, max_pages, pages->n_pages)) != AVTP_OK) return rc;
+  if (!cu_q || !kv_len || !block_table || !std::isfinite(softmax_scale) || softmax_scale <= 0.f)
+    return AVTP_ERR_INVALID_ARG;
+  if (N_q > 0 && (!rows_ok(q, q_stride, Hq, *pages) || !rows_ok(out, out_stride, Hq, *pages)))
+    return AVTP_ERR_INVALID_ARG;
+  const PageAttnPlan L = page_attn_plan(*pages, Hq, B, N_q, max_kv_len);
+  if (L.bytes > 0 && (!ws || ws_bytes < L.bytes || (uintptr_t)ws % 256)) return AVTP_ERR_WORKSPACE;
+  if (N_q == 0) return AVTP_OK;
+  const int64_t es = pages->dtype == AVTP_FP32 ? 4 : 2;
+  const PageAttnArgs A{q,      out,    q_stride * es, out_stride * es, lse, cu_q,      kv_len,
+                       block_table, status, B,        Hq,              (int)N_q, max_pages, softmax_scale};
+  return hip_status(launch_page_attention((hipStream_t)stream, *pages, L, A, (char *)ws));
 }
 
 }  // extern "C"

@@ -123,4 +123,45 @@ hipError_t launch_layer_attention(hipStream_t stream, const DevLayout &L, const 
 hipError_t launch_layer_select(hipStream_t stream, const float *A, int L, int N, int k,
                                int32_t *rank_sum, int32_t *selected);
 
+// The paged K/V cache: block tables and slots, pages handed back, rows stored.
+struct PageTables {
+  int B, page_shift, max_pages, n_pages;
+  const int32_t *seq_len;
+  const int32_t *free_count;
+  int32_t *seq_len_out, *free_count_out, *status;
+};
+hipError_t launch_page_tables(hipStream_t stream, const PageTables &P, const int32_t *cu_new,
+                              const int32_t *free_pages, int32_t *block_table, int32_t *slot_map,
+                              int64_t n_new);
+hipError_t launch_page_trim(hipStream_t stream, const PageTables &P, const int32_t *keep_len,
+                            const int32_t *block_table, int32_t *free_pages);
+hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void *k,
+                             int64_t k_stride_bytes, const void *v, int64_t v_stride_bytes,
+                             int64_t n_src, const int32_t *slot_map, const int32_t *keep_idx,
+                             int64_t n);
+
+// Attention over the pages: its launch, from host-known sizes only (so the
+// workspace size and the launch always agree).
+struct PageAttnPlan {
+  bool few;     // few rows per sequence: one row tile per block, its waves share out the keys
+  int tiles;    // row tile slots: every sequence's tiles have slots of their own
+  int nsplit;   // key ranges per row tile
+  int chunk;    // keys per range (the last one takes the rest)
+  size_t off_lse, bytes;  // partial rows [nsplit][N_q * Hq][d] fp32, then their log2 sums
+};
+PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len);
+
+struct PageAttnArgs {
+  const void *q;
+  void *out;
+  int64_t q_tok, out_tok;  // bytes from one token to the next
+  float *lse;
+  const int32_t *cu_q, *kv_len, *table;
+  int32_t *status;
+  int B, Hq, N_q, max_pages;
+  float scale;
+};
+hipError_t launch_page_attention(hipStream_t stream, const avtp_pages &P, const PageAttnPlan &L,
+                                 const PageAttnArgs &A, char *ws);
+
 }  // namespace avtp

@@ -8,7 +8,8 @@ hidden states; ``ProgressivePruner.step`` then prunes in VARIATION mode:
     score (1 - cos(h_cur, h_prior))  ->  budget  ->  select  ->  compact
 
 compacting h_cur together with the caller's other per-token tensors (position
-ids, the layer's K and V), and turns the kept tokens into the next layer's
+ids, the layer's K and V; with a PagedCache the kept K and V rows go straight
+into its pages instead), and turns the kept tokens into the next layer's
 layout.  The compacted h_cur is both the layer's output and the next pruning
 layer's h_prior.  Every step runs in libavtp.so; this module only sequences
 the calls, copies the new layout's small index arrays to the host (one
@@ -49,9 +50,13 @@ class ProgressivePruner:
             floor_abs, mode
 
     def step(self, h_cur: torch.Tensor, others: Sequence = (), keep_pct_next: int = 50,
-             status: torch.Tensor = None):
+             status: torch.Tensor = None, cache=None, k: torch.Tensor = None,
+             v: torch.Tensor = None, layer: int = 0):
         """Prune at one layer.  others: (tensor, token_dim) pairs compacted with
-        h_cur.  Returns (h_out, [compacted others], keep_idx, budget, scores, img_sum);
+        h_cur.  cache (a PagedCache with a row for every sequence of the batch)
+        takes the kept rows of the layer's k and v [N_tok, Hkv, d] behind what
+        its sequences hold already, into the pages of its layer ``layer``.
+        Returns (h_out, [compacted others], keep_idx, budget, scores, img_sum);
         afterwards self.dl is the next layer's layout (keep totals from
         keep_pct_next) and self.h_prior is h_out."""
         dl = self.dl
@@ -63,6 +68,8 @@ class ProgressivePruner:
             pairs.append((src, torch.empty(shape, dtype=src.dtype, device=src.device), tdim))
         bud, keep, cu_out = A.budget_select_compact(dl, isum, scores, pairs, self.alpha, self.lo, self.hi,
                                                     self.floor, mode=self.mode, status=status)
+        if cache is not None:
+            cache.store(layer, k, v, cache.reserve(cu_out, dl.N_out, status=status), keep_idx=keep)
         # (one synchronisation per pruning layer)
         self.dl = A.DeviceLayout.pruned(dl, keep, cu_out,
                                         lambda n, cu: keep_totals(n, cu, keep_pct_next))
