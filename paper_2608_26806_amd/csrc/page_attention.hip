@@ -42,10 +42,11 @@ typedef __amdgpu_buffer_rsrc_t Rsrc;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTile = 32;  // query rows and keys of an MFMA tile
-// The maximum a row's exponentials refer to is raised only when a logit
-// exceeds it by more than this (log2 units): probabilities up to 2^8 are as
-// good as those up to 1 in fp32 and in bf16, and most tiles then scale nothing.
-constexpr float kLazy = 8.f;
+// A row's exponentials refer to the largest logit m of some earlier tile, not
+// always of all: only when their sum over a tile leaves this range is m raised
+// (and the sum and output so far scaled).  fp32 sums, and products with bf16 or
+// fp32 probabilities of that size, are as exact as with the true maximum.
+constexpr float kLazyLimit = 65536.f;
 
 template <typename T, int D>
 struct Geo {
@@ -55,14 +56,12 @@ struct Geo {
   static constexpr int RPL = 64 / NCH;             // rows of a wave's load
   static constexpr int NS = D * (int)sizeof(T) / 32;  // K fragments per key (16 bytes per lane half)
   static constexpr int ND = D / 32;                // output tiles of 32 values
-  // Chunk order inside an LDS row, XOR-ed so that the rows an operand read
-  // touches lie in different banks.  K: 32 consecutive rows, one chunk.
-  static __device__ inline int kswz(int row) { return row & (NCH < 16 ? NCH - 1 : 15); }
-  // V, bf16: a transposing read takes four consecutive rows of 64 bytes (and
-  // the four rows behind them): they go to different 64-byte quarters of the
-  // banks.  fp32: 128 bytes of one row and of the row four further on.
-  static __device__ inline int vswz(int row) {
-    if (F32) return kswz(row);
+  // Chunk order inside an LDS row, XOR-ed with the row: 16 consecutive rows of
+  // one chunk (a K fragment) lie in 16 different places of the 64 banks, and so
+  // do the four 64-byte pieces of consecutive rows that a transposing read of
+  // bf16 V takes (with those of the next four rows in the other lane half).
+  static __device__ inline int swz(int row) {
+    if (F32) return row & 15;
     return NCH == 16 ? ((row & 3) << 2) | ((row >> 2) & 3) : (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
   }
 };
@@ -136,7 +135,7 @@ __device__ inline Seq find_seq(const KArgs &a, int slot, int bm_shift) {
 // stage.  WR = 1: few rows (a decode step), every wave streams keys of its
 // own and waits for nobody.
 template <typename T, int D, int WR, int WK, int TPW>
-__global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kernel(KArgs a) {
+__global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 2)) void page_attn_kernel(KArgs a) {
   using G_ = Geo<T, D>;
   constexpr bool F32 = G_::F32;
   constexpr int NW = WR * WK, BM = WR * kTile, ROWB = G_::ROWB, NCH = G_::NCH, RPL = G_::RPL;
@@ -208,13 +207,12 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
   }
 
   // where this lane's loads of a 16-row group come from
-  uint32_t voffk[LPG], voffv[LPG];
+  uint32_t voff[LPG];
   const int r0w = wave * RW;  // the wave's first row of a stage
 #pragma unroll
   for (int i = 0; i < LPG; ++i) {
     const int r = i * RPL + lane / NCH;
-    voffk[i] = (uint32_t)(r * ROWB + ((lane % NCH) ^ G_::kswz(r0w + r)) * 16);
-    voffv[i] = (uint32_t)(r * ROWB + ((lane % NCH) ^ G_::vswz(r0w + r)) * 16);
+    voff[i] = (uint32_t)(r * ROWB + ((lane % NCH) ^ G_::swz(r0w + r)) * 16);
   }
   const int32_t *trow = a.table + (long long)b * a.max_pages;
   const int pmask = (1 << a.page_shift) - 1;
@@ -238,10 +236,10 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
       char *dst = buf + (r0w + gi * 16) * ROWB;
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (AVTP_LDS void *)(dst + i * 1024), 16, (int)voffk[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (AVTP_LDS void *)(dst + i * 1024), 16, (int)voff[i], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (AVTP_LDS void *)(dst + TB + i * 1024), 16, (int)voffv[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (AVTP_LDS void *)(dst + TB + i * 1024), 16, (int)voff[i], 0, 0, 0);
     }
   };
 
@@ -254,25 +252,35 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
   // element e of a tile of this lane: key eoff(e) + 4 hi of the tile
   auto eoff = [](int e) __attribute__((always_inline)) { return 8 * (e >> 2) + (e & 3); };
 
-  // A part of V's operand: value 32 dt + col of the keys the lane's
-  // probabilities 8 c .. 8 c + 7 belong to (bf16), or of key eoff(e) + 4 hi (fp32)
+  // LDS addresses of a tile's operands: the lane's base, XOR-ed with the chunk,
+  // plus rows that fit the instruction's offset.
+  // K: row col, fragment s
+  typedef AVTP_LDS const char *lptr;
+  const uint32_t kbase = (uint32_t)(col * ROWB + ((hi ^ G_::swz(col)) << 4));
+  auto kaddr = [&](lptr kt, int s) __attribute__((always_inline)) { return kt + (kbase ^ (uint32_t)(s << 5)); };
+  // V, bf16: the transposing read hands lane i of 16 the value i of four rows of
+  // 16 values whose addresses the lanes give (lane i: four values of row i / 4),
+  // here 32 dt + col of the four keys 16 c + 8 j + 4 hi + .. that belong to the
+  // lane's probabilities 8 c + 4 j + ..
   const int ti = lane & 15, tq = (lane >> 4) & 1;
-  auto vfrag = [&](const char *vt, int c, int dt) __attribute__((always_inline)) {
+  const int vrow = F32 ? 4 * hi : 4 * hi + (ti >> 2);
+  const uint32_t vbase = F32 ? (uint32_t)(vrow * ROWB + (((col >> 2) ^ G_::swz(vrow)) << 4) + (col & 3) * 4)
+                             : (uint32_t)(vrow * ROWB + (((2 * tq + ((ti & 3) >> 1)) ^ G_::swz(vrow)) << 4) + (ti & 1) * 8);
+  auto vfrag = [&](lptr vt, int c, int dt) __attribute__((always_inline)) {
     bf16x8 f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const int r = 16 * c + 8 * j + 4 * hi + (ti >> 2);
-      const int ch = 4 * dt + 2 * tq + ((ti & 3) >> 1);
-      const char *p = vt + r * ROWB + ((ch ^ G_::vswz(r)) << 4) + (ti & 1) * 8;
-      const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((AVTP_LDS bf16x4 *)p);
+      const uint32_t o = (vbase ^ (uint32_t)(dt << 6 | (G_::swz(8 * j) << 4))) + (uint32_t)((16 * c + 8 * j) * ROWB);
+      const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((AVTP_LDS bf16x4 *)(vt + o));
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[4 * j + i] = x[i];
     }
     return f;
   };
-  auto velem = [&](const char *vt, int r, int dt) __attribute__((always_inline)) {
-    const int ch = 8 * dt + (col >> 2);
-    return *reinterpret_cast<const float *>(vt + r * ROWB + ((ch ^ G_::vswz(r)) << 4) + (col & 3) * 4);
+  // fp32: value 32 dt + col of key eoff(e) + 4 hi
+  auto velem = [&](lptr vt, int e, int dt) __attribute__((always_inline)) {
+    const uint32_t o = (vbase ^ (uint32_t)(((8 * dt) ^ G_::swz(eoff(e))) << 4)) + (uint32_t)(eoff(e) * ROWB);
+    return *reinterpret_cast<AVTP_LDS const float *>(vt + o);
   };
 
   // Values of V that are not finite, in a tile that some row sees only in
@@ -281,17 +289,17 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
   auto not_finite = [&](uint32_t x) __attribute__((always_inline)) {
     return F32 ? (x & 0x7f800000u) == 0x7f800000u : ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0u);
   };
-  auto tile_not_finite = [&](const char *vt) __attribute__((always_inline)) {
+  auto tile_not_finite = [&](lptr vt) __attribute__((always_inline)) {
     bool bad = false;
 #pragma unroll
     for (int i = 0; i < kTile * NCH / 64; ++i) {
-      const u32x4 x = *reinterpret_cast<const u32x4 *>(vt + (i * 64 + lane) * 16);
+      const u32x4 x = *reinterpret_cast<AVTP_LDS const u32x4 *>(vt + (i * 64 + lane) * 16);
 #pragma unroll
       for (int j = 0; j < 4; ++j) bad = bad || not_finite(x[j]);
     }
     return __ballot(bad) != 0ull;
   };
-  auto add_not_finite = [&](const char *vt, int kb) __attribute__((always_inline)) {
+  auto add_not_finite = [&](lptr vt, int kb) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int r = 0; r < kTile; ++r) {
       const bool seen = kb + r < lim;
@@ -302,7 +310,7 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
           const int dd = 32 * dt + eoff(e) + 4 * hi;  // this lane's value of the output
           const int ch = dd * (int)sizeof(T) / 16, by = dd * (int)sizeof(T) % 16;
           const float x =
-              (float)*reinterpret_cast<const T *>(vt + r * ROWB + ((ch ^ G_::vswz(r)) << 4) + by);
+              (float)*reinterpret_cast<AVTP_LDS const T *>(vt + r * ROWB + ((ch ^ G_::swz(r)) << 4) + by);
           const bool add = seen && !(__builtin_fabsf(x) < INFINITY);
           O[dt][e] += add ? x : 0.f;
         }
@@ -310,79 +318,116 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
     }
   };
 
-  // One tile of 32 keys from key kb on: kt and vt are its first rows
-  auto tile = [&](const char *kt, const char *vt, int kb, auto masked_tag) __attribute__((always_inline)) {
-    constexpr bool MASKED = decltype(masked_tag)::value;
+  // S^T of the 32 keys at kt
+  auto logits = [&](lptr kt) __attribute__((always_inline)) {
     f32x16 S = f32x16{};
 #pragma unroll
     for (int s = 0; s < NS; ++s) {
-      const char *p = kt + col * ROWB + (((2 * s + hi) ^ G_::kswz(col)) << 4);
       if constexpr (F32) {
-        const f32x4 kf = *reinterpret_cast<const f32x4 *>(p), qv = __builtin_bit_cast(f32x4, qf[s]);
+        const f32x4 kf = *reinterpret_cast<AVTP_LDS const f32x4 *>(kaddr(kt, s)), qv = __builtin_bit_cast(f32x4, qf[s]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qv[i], S, 0, 0, 0);
       } else {
-        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8 *>(p),
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<AVTP_LDS const bf16x8 *>(kaddr(kt, s)),
                                                     __builtin_bit_cast(bf16x8, qf[s]), S, 0, 0, 0);
       }
     }
-    if constexpr (MASKED) {
+    return S;
+  };
+  // p = 2^(c S - m), as the second product takes them, and their sum
+  struct Bf {
+    bf16x8 x[2];
+  };
+  typedef std::conditional_t<F32, f32x16, Bf> Probs;
+  auto probs = [&](const f32x16 &S, Probs &p, float ref) __attribute__((always_inline)) {
+    float sum[2];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) S[e] = kb + 4 * hi + eoff(e) < lim ? S[e] : -INFINITY;
+    for (int e = 0; e < 16; ++e) {
+      const float x = __builtin_amdgcn_exp2f(S[e] * cl2e - ref);
+      sum[e & 1] = e < 2 ? x : sum[e & 1] + x;
+      if constexpr (F32) p[e] = x;
+      else p.x[e >> 3][e & 7] = (__bf16)x;
     }
+    return sum[0] + sum[1];
+  };
+  // a row's sum of a tile left its range (or there is no reference yet): its
+  // reference becomes the largest logit, its sum and output are scaled
+  auto raise = [&](const f32x16 &S, float t) __attribute__((always_inline)) {
     float top = S[0];
 #pragma unroll
     for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
     top = half_max(top) * cl2e;
-    if (__ballot(top > m + kLazy) != 0ull) {
-      const float nm = fmaxf(m, top);
-      const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
-      m = nm;
-      l *= f;
+    const bool bad = half_max(t <= kLazyLimit ? 0.f : 1.f) > 0.f;  // (both lanes of the row alike)
+    const float nm = bad ? fmaxf(m, top) : m;
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
+    m = nm;
+    l *= f;
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt)
+    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) O[dt][e] *= f;
-    }
-    const float ref = m == -INFINITY ? 0.f : m;  // (no key seen so far: every term is 0)
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      S[e] = __builtin_amdgcn_exp2f(S[e] * cl2e - ref);
-      sum[e & 1] += S[e];
-    }
-    l += sum[0] + sum[1];
-    bool clean = false;
-    if constexpr (MASKED) {
-      clean = tile_not_finite(vt);
-      if (clean) add_not_finite(vt, kb);
-    }
+      for (int e = 0; e < 16; ++e) O[dt][e] *= f;
+  };
+  // O^T += V^T P^T
+  auto weigh = [&](lptr vt, const Probs &p, bool clean) __attribute__((always_inline)) {
     if constexpr (F32) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-          float x = velem(vt, eoff(e) + 4 * hi, dt);
-          if (MASKED && clean) x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
-          O[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, S[e], O[dt], 0, 0, 0);
+          float x = velem(vt, e, dt);
+          if (clean) x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
+          O[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[e], O[dt], 0, 0, 0);
         }
       }
     } else {
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
-        bf16x8 p;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = (__bf16)S[8 * c + i];
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
           bf16x8 f = vfrag(vt, c, dt);
-          if (MASKED && clean) {
+          if (clean) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = __builtin_fabsf((float)f[i]) < INFINITY ? f[i] : (__bf16)0.f;
           }
-          O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p, O[dt], 0, 0, 0);
+          O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p.x[c], O[dt], 0, 0, 0);
         }
       }
+    }
+  };
+  // N tiles of 32 keys that every row of the wave sees
+  auto whole = [&](lptr kt, lptr vt, auto n_tag) __attribute__((always_inline)) {
+    constexpr int N = decltype(n_tag)::value;
+    f32x16 S[N];
+    Probs p[N];
+    float tot = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) S[i] = logits(kt + i * kTile * ROWB);
+#pragma unroll
+    for (int i = 0; i < N; ++i) tot += probs(S[i], p[i], m);
+    if (__ballot(!(tot <= kLazyLimit)) != 0ull) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) raise(S[i], tot);
+      tot = 0.f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) tot += probs(S[i], p[i], m == -INFINITY ? 0.f : m);  // (-inf: no other logits)
+    }
+    l += tot;
+#pragma unroll
+    for (int i = 0; i < N; ++i) weigh(vt + i * kTile * ROWB, p[i], false);
+  };
+  // a tile of keys from kb on of which some rows see a part
+  auto part = [&](lptr kt, lptr vt, int kb) __attribute__((always_inline)) {
+    f32x16 S = logits(kt);
+    Probs p;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) S[e] = kb + 4 * hi + eoff(e) < lim ? S[e] : -INFINITY;
+    raise(S, INFINITY);
+    l += probs(S, p, m == -INFINITY ? 0.f : m);  // (no key seen so far: every term is 0)
+    if (tile_not_finite(vt)) {
+      add_not_finite(vt, kb);
+      weigh(vt, p, true);
+    } else {
+      weigh(vt, p, false);
     }
   };
 
@@ -398,14 +443,15 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 ? 1 : 2)) void page_attn_kern
       issue(nxt, ks + KS, ids);
       ids = load_ids(ks + 2 * KS);
     }
-#pragma unroll
-    for (int t = 0; t < TPW; ++t) {
-      const int r = (wk * TPW + t) * kTile, kb = ks + r;
-      // keys of the tile below the range's end, and the rows that see them
-      if (kb >= min(kend, wmax)) break;
-      const char *kt = buf + r * ROWB, *vt = kt + TB;
-      if (kb + kTile <= min(kend, wmin)) tile(kt, vt, kb, std::false_type{});
-      else tile(kt, vt, kb, std::true_type{});
+    // keys of this wave below the range's end, and the rows that see them
+    const int kb = ks + wk * TPW * kTile, stop = min(kend, wmax);
+    lptr kt = (lptr)(buf) + wk * TPW * kTile * ROWB, vt = kt + TB;
+    if (kb + TPW * kTile <= min(kend, wmin)) {
+      whole(kt, vt, std::integral_constant<int, TPW>{});
+    } else {
+#pragma unroll 1
+      for (int t = 0; t < TPW; ++t)
+        if (kb + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, kb + t * kTile);
     }
   };
   for (int st = 0; st < nstage; st += 2) {
