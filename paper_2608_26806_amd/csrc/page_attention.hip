@@ -77,6 +77,16 @@ struct KArgs {
   float cl2e;
 };
 
+// A buffer of `bytes` bytes at p, both the same in every lane (said once more
+// here: left to the compiler's analysis, every load became a loop over lanes).
+__device__ inline Rsrc make_rsrc(const char *p, int bytes) {
+  const unsigned long long u = (unsigned long long)p;
+  const unsigned long long lo = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)u);
+  const unsigned long long hi = (unsigned)__builtin_amdgcn_readfirstlane((int)(unsigned)(u >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc((void *)(lo | hi << 32), 0, __builtin_amdgcn_readfirstlane(bytes),
+                                           0x00027000);
+}
+
 __device__ inline void wait_vmem() {
   __builtin_amdgcn_s_waitcnt(0xF70);
   asm volatile("" ::: "memory");
@@ -231,8 +241,7 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
       if (!ok && key < L && a.status && lane == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
       const int have = ok ? min(max(L - key, 0), GR) * ROWB : 0;
       const long long off = ok ? ((long long)id * a.Hkv + g) * a.head_bytes + (long long)(key & pmask) * ROWB : 0;
-      const Rsrc rk = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a.k + off), 0, have, 0x00027000);
-      const Rsrc rv = __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(a.v + off), 0, have, 0x00027000);
+      const Rsrc rk = make_rsrc(a.k + off, have), rv = make_rsrc(a.v + off, have);
       char *dst = buf + (r0w + gi * 16) * ROWB;
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
@@ -350,23 +359,6 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
     }
     return sum[0] + sum[1];
   };
-  // a row's sum of a tile left its range (or there is no reference yet): its
-  // reference becomes the largest logit, its sum and output are scaled
-  auto raise = [&](const f32x16 &S, float t) __attribute__((always_inline)) {
-    float top = S[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
-    top = half_max(top) * cl2e;
-    const bool bad = half_max(t <= kLazyLimit ? 0.f : 1.f) > 0.f;  // (both lanes of the row alike)
-    const float nm = bad ? fmaxf(m, top) : m;
-    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
-    m = nm;
-    l *= f;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) O[dt][e] *= f;
-  };
   // O^T += V^T P^T
   auto weigh = [&](lptr vt, const Probs &p, bool clean) __attribute__((always_inline)) {
     if constexpr (F32) {
@@ -394,7 +386,8 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
       }
     }
   };
-  // N tiles of 32 keys that every row of the wave sees
+  // N tiles of 32 keys that every row of the wave sees.  false (nothing done):
+  // a row's sum left its range, or has no reference yet; `part` takes them.
   auto whole = [&](lptr kt, lptr vt, auto n_tag) __attribute__((always_inline)) {
     constexpr int N = decltype(n_tag)::value;
     f32x16 S[N];
@@ -404,26 +397,32 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
     for (int i = 0; i < N; ++i) S[i] = logits(kt + i * kTile * ROWB);
 #pragma unroll
     for (int i = 0; i < N; ++i) tot += probs(S[i], p[i], m);
-    if (__ballot(!(tot <= kLazyLimit)) != 0ull) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) raise(S[i], tot);
-      tot = 0.f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) tot += probs(S[i], p[i], m == -INFINITY ? 0.f : m);  // (-inf: no other logits)
-    }
+    if (__builtin_expect(__ballot(!(tot <= kLazyLimit)) != 0ull, 0)) return false;
     l += tot;
 #pragma unroll
     for (int i = 0; i < N; ++i) weigh(vt + i * kTile * ROWB, p[i], false);
+    return true;
   };
-  // a tile of keys from kb on of which some rows see a part
+  // A tile of keys from kb on, of which some rows may see a part or nothing, and
+  // whose largest logit becomes the row's reference if it is larger.
   auto part = [&](lptr kt, lptr vt, int kb) __attribute__((always_inline)) {
     f32x16 S = logits(kt);
     Probs p;
 #pragma unroll
     for (int e = 0; e < 16; ++e) S[e] = kb + 4 * hi + eoff(e) < lim ? S[e] : -INFINITY;
-    raise(S, INFINITY);
+    float top = S[0];
+#pragma unroll
+    for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
+    const float nm = fmaxf(m, half_max(top) * cl2e);
+    const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
+    m = nm;
+    l *= f;
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) O[dt][e] *= f;
     l += probs(S, p, m == -INFINITY ? 0.f : m);  // (no key seen so far: every term is 0)
-    if (tile_not_finite(vt)) {
+    if (__builtin_expect(tile_not_finite(vt), 0)) {
       add_not_finite(vt, kb);
       weigh(vt, p, true);
     } else {
@@ -446,13 +445,12 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
     // keys of this wave below the range's end, and the rows that see them
     const int kb = ks + wk * TPW * kTile, stop = min(kend, wmax);
     lptr kt = (lptr)(buf) + wk * TPW * kTile * ROWB, vt = kt + TB;
-    if (kb + TPW * kTile <= min(kend, wmin)) {
-      whole(kt, vt, std::integral_constant<int, TPW>{});
-    } else {
+    if (__builtin_expect(kb + TPW * kTile <= min(kend, wmin), 1) &&
+        __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
+      return;
 #pragma unroll 1
-      for (int t = 0; t < TPW; ++t)
-        if (kb + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, kb + t * kTile);
-    }
+    for (int t = 0; t < TPW; ++t)
+      if (kb + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, kb + t * kTile);
   };
   for (int st = 0; st < nstage; st += 2) {
     step(smA, smB, st);
