@@ -143,11 +143,12 @@ hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void
 // Attention over the pages: its launch, from host-known sizes only (so the
 // workspace size and the launch always agree).
 struct PageAttnPlan {
-  bool few;     // few rows per sequence: one row tile per block, its waves share out the keys
-  int tiles;    // row tile slots: every sequence's tiles have slots of their own
-  int nsplit;   // key ranges per row tile
-  int chunk;    // keys per range (the last one takes the rest)
-  size_t off_lse, bytes;  // partial rows [nsplit][N_q * Hq][d] fp32, then their log2 sums
+  bool few;        // few rows per sequence: tiles of 32 rows, else of 128
+  int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
+  int nsplit;      // many: key ranges per tile
+  int least;       // few: units (32 keys of a tile) per worker, many: keys per range, at least
+  int cuts;        // tiles that may have been cut, and how many parts they may leave:
+  size_t off_lse, off_meta, bytes;  // rows fp32, their log2 sums, whose they are
 };
 PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len);
 

@@ -26,6 +26,7 @@
 #include <type_traits>
 
 #include "avtp_internal.h"
+#include "wave_ops.h"
 
 namespace avtp {
 namespace {
@@ -66,6 +67,19 @@ struct Geo {
   }
 };
 
+// values dd .. dd + 3 of an output row
+template <typename T>
+__device__ inline void put4(char *row, int dd, f32x4 x) {
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<f32x4 *>(row + dd * 4) = x;
+  } else {
+    bf16x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (__bf16)x[i];
+    *reinterpret_cast<bf16x4 *>(row + dd * 2) = y;
+  }
+}
+
 struct KArgs {
   const char *q, *k, *v;
   char *out;
@@ -73,7 +87,9 @@ struct KArgs {
   float *lse, *po, *pl;
   const int32_t *cu_q, *kv_len, *table;
   int32_t *status;
-  int B, Hq, Hkv, G, N_q, max_pages, n_pages, page_shift, nsplit, chunk;
+  int B, Hq, Hkv, G, N_q, max_pages, n_pages, page_shift;
+  int workers, nsplit, least;  // see PageAttnPlan
+  int4 *meta;                  // two per possible cut tile
   float cl2e;
 };
 
@@ -104,117 +120,196 @@ __device__ inline float half_sum(float x) {
   return __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
 }
 
-// Row tile slots: sequence b's tiles of BM rows are numbered from
-// floor(cu_q[b] G / BM) + b on.  The next sequence's start is at least
-// ceil(n_b G / BM) further, so every tile has a slot of its own, there are at
-// most floor(N_q G / BM) + B, and no prefix sum is needed to find one.
+// The work.  A row tile is BM rows (token, head of the group) of one sequence
+// and key head; a unit is one stage of KS keys of a tile, and a tile has the
+// units of the keys its last row sees (one at least).  All units stand in one
+// line, key head by key head, sequence by sequence, tile by tile, and every
+// worker (block) takes the same number of them, so that long and short
+// sequences, causal tiles and few rows alike keep all of the chip busy to the
+// end.  A worker finds its first unit from the lengths alone.  A tile that the
+// line cuts leaves parts in the workspace, which page_join_kernel joins.  (With
+// one block per tile and key range, eight requests' chunks over 1,000 to 12,000
+// keys took 473 us, 64 requests' decode step 214.)
 struct Seq {
-  int b, q0, q1, kv, base;
+  int q0, n, kv, L;  // first row, new tokens, cached tokens, those the table has room for
 };
-__device__ inline Seq find_seq(const KArgs &a, int slot, int bm_shift) {
-  const int lane = threadIdx.x & 63;
-  auto first = [&](int c, int b) __attribute__((always_inline)) {
-    return ((min(max(0, c), a.N_q) * a.G) >> bm_shift) + b;
-  };
-  int w0 = 0;
-  if (a.B > 64) {
-    int step = 64;
-    while (step * 64 < a.B) step *= 64;
-    for (; step > 1; step >>= 6) {
-      const int c = w0 + lane * step;
-      const unsigned long long m = __ballot(c < a.B && first(a.cu_q[min(c, a.B)], c) <= slot);
-      w0 += max(0, __builtin_popcountll(m) - 1) * step;
-    }
-  }
-  const int c = min(w0 + lane, a.B - 1);
-  const int lo = a.cu_q[c], hi = a.cu_q[c + 1], kv = a.kv_len[c];
-  const unsigned long long m = __ballot(w0 + lane < a.B && first(lo, c) <= slot);
-  const int src = max(0, __builtin_popcountll(m) - 1);
+__device__ inline Seq seq_of(const KArgs &a, int b) {
   Seq s;
-  s.b = w0 + src;
-  s.q0 = min(max(0, __builtin_amdgcn_readlane(lo, src)), a.N_q);
-  s.q1 = min(max(s.q0, __builtin_amdgcn_readlane(hi, src)), a.N_q);
-  s.kv = max(0, __builtin_amdgcn_readlane(kv, src));
-  s.base = first(s.q0, s.b);
+  s.q0 = min(max(0, a.cu_q[b]), a.N_q);
+  s.n = min(max(s.q0, a.cu_q[b + 1]), a.N_q) - s.q0;
+  s.kv = max(0, a.kv_len[b]);
+  s.L = (int)min((long long)s.kv, (long long)a.max_pages << a.page_shift);
   return s;
 }
+__device__ inline Seq uniform(const Seq &s, int src) {
+  return {__builtin_amdgcn_readlane(s.q0, src), __builtin_amdgcn_readlane(s.n, src),
+          __builtin_amdgcn_readlane(s.kv, src), __builtin_amdgcn_readlane(s.L, src)};
+}
+template <int BM>
+__device__ inline int tiles_of(const KArgs &a, const Seq &s) {
+  return (s.n * a.G + BM - 1) / BM;
+}
+// keys that the last row of a tile sees
+template <int BM>
+__device__ inline int tile_keys(const KArgs &a, const Seq &s, int tile) {
+  return min(s.L, s.kv - s.n + (min((tile + 1) * BM, s.n * a.G) - 1) / a.G + 1);
+}
+template <int BM, int KS>
+__device__ inline int units_of(const KArgs &a, const Seq &s, int tile) {
+  return max(1, (tile_keys<BM>(a, s, tile) + KS - 1) / KS);
+}
+typedef uint64_t u64;
+// inclusive, over the lanes; v below 2^50
+__device__ inline u64 prefix_sum64(u64 v) {
+  return (u64)wave::prefix_sum((uint32_t)(v & 0xFFFFFF)) + ((u64)wave::prefix_sum((uint32_t)(v >> 24)) << 24);
+}
+// Units of lane i's sequence c0 + i (0 behind the last); every lane calls it.
+template <int BM, int KS>
+__device__ inline u64 seq_units(const KArgs &a, int c0, Seq &s) {
+  const int lane = threadIdx.x & 63, b = c0 + lane;
+  s = seq_of(a, min(b, a.B - 1));
+  const int T = b < a.B ? tiles_of<BM>(a, s) : 0;
+  constexpr int kAlone = 4;  // tiles that a lane sums by itself; more are spread over the wave
+  u64 w = 0;
+  for (int t = 0; t < min(T, kAlone); ++t) w += units_of<BM, KS>(a, s, t);
+  for (u64 m = __ballot(T > kAlone); m != 0; m &= m - 1) {
+    const int src = __builtin_ctzll(m), n = __builtin_amdgcn_readlane(T, src);
+    const Seq x = uniform(s, src);
+    u64 sum = 0;
+    for (int t = kAlone + lane; t < n; t += 64) sum += units_of<BM, KS>(a, x, t);
+    sum = wave::sum(sum);
+    if (lane == src) w += sum;
+  }
+  return w;
+}
 
-// A block takes one row tile (WR waves of 32 rows) of one key head and one
-// range of its keys; the keys of a stage are shared out over WK waves, whose
-// results are joined at the end.  WK = 1: many rows, the waves share every
-// stage.  WR = 1: few rows (a decode step), every wave streams keys of its
-// own and waits for nobody.
-template <typename T, int D, int WR, int WK, int TPW>
-__global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 2)) void page_attn_kernel(KArgs a) {
+// A place in the line of units: unit u of the U of tile t of sequence b and
+// key head g.  Wave-uniform, found by every wave for itself.
+template <int BM, int KS>
+struct Place {
+  int g, b, t, u, U;
+  Seq s;
+  // the place of unit w of the `per` units of a key head (first: the first 64
+  // sequences' units and descriptions)
+  __device__ inline void find(const KArgs &a, u64 w, u64 per, u64 units, const Seq &first) {
+    const int lane = threadIdx.x & 63;
+    g = (int)(w / per);
+    u64 r = w - (u64)g * per;
+    Seq sl = first;
+    int c0 = 0;
+    u64 incl = prefix_sum64(units);
+    for (;; c0 += 64) {
+      const u64 total = wave::lane_value(incl, 63);
+      if (r < total || c0 + 64 >= a.B) break;
+      r -= total;
+      units = seq_units<BM, KS>(a, c0 + 64, sl);
+      incl = prefix_sum64(units);
+    }
+    const int src = __builtin_ctzll(__ballot(r < incl) | 1ull << 63);
+    r -= wave::lane_value(incl - units, src);
+    b = c0 + src;
+    s = uniform(sl, src);
+    const int T = tiles_of<BM>(a, s);
+    for (t = 0;; t += 64) {  // 64 tiles at a time
+      const int x = t + lane < T ? units_of<BM, KS>(a, s, t + lane) : 0;
+      const u64 in = prefix_sum64(x), total = wave::lane_value(in, 63);
+      if (r >= total && t + 64 < T) {
+        r -= total;
+        continue;
+      }
+      const int k = __builtin_ctzll(__ballot(r < in) | 1ull << 63);
+      u = (int)(r - wave::lane_value(in - x, k));
+      U = __builtin_amdgcn_readlane(x, k);
+      t += k;
+      break;
+    }
+  }
+  // the first unit of the next tile (there is one)
+  __device__ inline void next(const KArgs &a) {
+    u = 0;
+    if (++t >= tiles_of<BM>(a, s)) {
+      t = 0;
+      const int lane = threadIdx.x & 63;
+      int c0 = b + 1;
+      for (;; c0 += 64) {
+        if (c0 >= a.B) {
+          ++g;
+          c0 = 0;
+        }
+        const Seq x = seq_of(a, min(c0 + lane, a.B - 1));
+        const u64 m = __ballot(c0 + lane < a.B && x.n > 0);
+        if (m != 0) {
+          const int src = __builtin_ctzll(m);
+          b = c0 + src;
+          s = uniform(x, src);
+          break;
+        }
+      }
+    }
+    U = units_of<BM, KS>(a, s, t);
+  }
+};
+
+// A tile that is cut: its parts' slots in the workspace are `first`, then `next`,
+// next + step, ..; `more` follow the first.  The block that takes its first
+// keys says so here (more = 0: nothing to join).
+struct Cut {
+  int more, g, q0, n, row0, first, next, step;
+};
+__device__ inline void put_cut(int4 *meta, int i, const Cut &c) {
+  meta[2 * i] = make_int4(c.more, c.g, c.q0, c.n);
+  meta[2 * i + 1] = make_int4(c.row0, c.first, c.next, c.step);
+}
+__device__ inline Cut get_cut(const int4 *meta, int i) {
+  const int4 x = meta[2 * i], y = meta[2 * i + 1];
+  return {x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
+}
+
+// One tile (or, cut, some of its keys): the rows row0 .. of sequence b and key
+// head g over keys kbeg .. kend - 1.
+struct Job {
+  int g, b, row0, kbeg, kend, slot;  // slot: where a cut tile's part goes
+  bool cut;
+  Seq s;
+};
+
+// WR waves of 32 rows each share the stages of TPW tiles of 32 keys.
+template <typename T, int D, int WR, int TPW>
+struct Shape {
   using G_ = Geo<T, D>;
+  static constexpr int BM = WR * kTile;
+  static constexpr int KS = TPW * kTile;           // keys per stage
+  static constexpr int RW = KS / WR;               // of them, rows a wave loads
+  static constexpr int GR = RW < 16 ? RW : 16;     // rows of one page group
+  static constexpr int NG = RW / GR, LPG = GR / G_::RPL;
+  static_assert(RW % G_::RPL == 0 && GR % G_::RPL == 0, "whole loads");
+  static constexpr int TB = KS * G_::ROWB;         // bytes of one tensor's stage
+  // two waves per SIMD, one where the registers of an fp32 tile leave room for one
+  static constexpr int kPerSimd = G_::ROWB > 256 ? 1 : 2;
+};
+
+template <typename T, int D, int WR, int TPW>
+__device__ __attribute__((always_inline)) inline void attend(const KArgs &a, const Job &job, AVTP_LDS char *bufA,
+                                                             AVTP_LDS char *bufB) {
+  using G_ = Geo<T, D>;
+  using S_ = Shape<T, D, WR, TPW>;
   constexpr bool F32 = G_::F32;
-  constexpr int NW = WR * WK, BM = WR * kTile, ROWB = G_::ROWB, NCH = G_::NCH, RPL = G_::RPL;
-  constexpr int NS = G_::NS, ND = G_::ND;
-  constexpr int KS = WK * TPW * kTile;             // keys per stage
-  constexpr int RW = KS / NW;                      // of them, rows a wave loads (its own, if WK > 1)
-  constexpr int GR = RW < 16 ? RW : 16;            // rows of one page group
-  constexpr int NG = RW / GR, LPG = GR / RPL;
-  static_assert(WR == 1 || WK == 1, "");
-  static_assert(RW % RPL == 0 && GR % RPL == 0 && (WK == 1 || RW == TPW * kTile), "whole loads");
-  constexpr int TB = KS * ROWB;                    // bytes of one tensor's stage
-  // two stage buffers as distinct objects, so the compiler can tell the one
-  // being read from the one in flight
-  __shared__ __attribute__((aligned(16))) char smA[2 * TB];
-  __shared__ __attribute__((aligned(16))) char smB[2 * TB];
-  __shared__ float ml_s[WK > 1 ? WK * kTile * 2 : 1];
-
+  constexpr int BM = S_::BM, KS = S_::KS, RW = S_::RW, GR = S_::GR, NG = S_::NG, LPG = S_::LPG, TB = S_::TB;
+  constexpr int ROWB = G_::ROWB, NCH = G_::NCH, RPL = G_::RPL, NS = G_::NS, ND = G_::ND;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wr = WR > 1 ? wave : 0, wk = WK > 1 ? wave : 0;
+  const int wave = WR > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
   const int hi = lane >> 5, col = lane & 31;
-  constexpr int kBmShift = BM == 32 ? 5 : (BM == 128 ? 7 : 8);
-  static_assert(BM == 1 << kBmShift, "");
-
-  // key heads fastest: blocks go to the XCDs in turn, so an XCD sees few heads.
-  // The last tiles of a sequence see the most keys and go first.
-  const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
-  const int nslots = gridDim.x / a.Hkv / a.nsplit;
-  const int slot = nslots - 1 - rest / a.nsplit, split = rest % a.nsplit;
-  const Seq sq = find_seq(a, slot, kBmShift);
-  const int b = sq.b, n = sq.q1 - sq.q0;
-  const int R = n * a.G, row0 = (slot - sq.base) * BM;
-  if (slot < sq.base || row0 >= R) return;
-
-  // tokens of the sequence that the table has room for
-  const long long cap = (long long)a.max_pages << a.page_shift;
-  const int L = (int)min((long long)sq.kv, cap);
-  if (L < sq.kv && a.status && tid == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
+  const float cl2e = a.cl2e;
+  const int pmask = (1 << a.page_shift) - 1;
+  const int g = job.g, b = job.b, L = job.s.L, row0 = job.row0, kbeg = job.kbeg, kend = job.kend;
+  const int R = job.s.n * a.G;
+  if (L < job.s.kv && a.status && tid == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
   // row r of the sequence: token r / G, which sees kv - n + token + 1 keys
-  const int wrow = row0 + wr * kTile;
+  const int wrow = row0 + wave * kTile;
   const int row = min(wrow + col, R - 1), tok = row / a.G, head = g * a.G + (row - tok * a.G);
-  const int lim = min(L, sq.kv - n + tok + 1);
+  const int lim = min(L, job.s.kv - job.s.n + tok + 1);
   const bool valid = wrow + col < R;
   const int wmin = __builtin_amdgcn_readlane(lim, 0), wmax = __builtin_amdgcn_readlane(lim, 31);
-  const int blast = min(row0 + BM, R) - 1;
-  const int bmax = min(L, sq.kv - n + blast / a.G + 1);  // keys the block's last row sees
-  const int kbeg = split * a.chunk;
-  const int kend = split + 1 < a.nsplit ? min(bmax, kbeg + a.chunk) : bmax;
-
-  // (a row's place among all rows: token, then head)
-  const long long orow = (long long)(sq.q0 + tok) * a.Hq + head;
-  if (kbeg >= kend) {  // no key for any row of the block
-    if (a.nsplit > 1) {
-      if (wk == 0 && valid && hi == 0) a.pl[(long long)split * a.N_q * a.Hq + orow] = -INFINITY;
-    } else if (wk == 0 && valid) {
-      u32x4 *o = reinterpret_cast<u32x4 *>(a.out + (sq.q0 + tok) * a.out_tok + (long long)head * ROWB);
-      for (int c = hi; c < NCH; c += 2) o[c] = u32x4{};
-      if (a.lse && hi == 0) a.lse[(long long)head * a.N_q + sq.q0 + tok] = -INFINITY;
-    }
-    return;
-  }
-
-  // query rows, the second operand of S^T
-  u32x4 qf[NS];
-  {
-    const char *p = a.q + (sq.q0 + tok) * a.q_tok + (long long)head * ROWB + hi * 16;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(p + s * 32);
-  }
 
   // where this lane's loads of a 16-row group come from
   uint32_t voff[LPG];
@@ -224,15 +319,23 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
     const int r = i * RPL + lane / NCH;
     voff[i] = (uint32_t)(r * ROWB + ((lane % NCH) ^ G_::swz(r0w + r)) * 16);
   }
+
+  // query rows, the second operand of S^T
+  u32x4 qf[NS];
+  {
+    const char *p = a.q + (job.s.q0 + tok) * a.q_tok + (long long)head * ROWB + hi * 16;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(p + s * 32);
+  }
+
   const int32_t *trow = a.table + (long long)b * a.max_pages;
-  const int pmask = (1 << a.page_shift) - 1;
   // page ids of the wave's groups of the stage at key ks, one per lane (lane
   // gi: group gi), read a stage ahead
   auto load_ids = [&](int ks) __attribute__((always_inline)) {
     const int key = min(ks + r0w + (lane & (NG - 1)) * 16, L - 1);
     return trow[key >> a.page_shift];
   };
-  auto issue = [&](char *buf, int ks, int ids) __attribute__((always_inline)) {
+  auto issue = [&](AVTP_LDS char *buf, int ks, int ids) __attribute__((always_inline)) {
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int id = __builtin_amdgcn_readlane(ids, gi);
@@ -242,13 +345,13 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
       const int have = ok ? min(max(L - key, 0), GR) * ROWB : 0;
       const long long off = ok ? ((long long)id * a.Hkv + g) * a.head_bytes + (long long)(key & pmask) * ROWB : 0;
       const Rsrc rk = make_rsrc(a.k + off, have), rv = make_rsrc(a.v + off, have);
-      char *dst = buf + (r0w + gi * 16) * ROWB;
+      AVTP_LDS char *dst = buf + (r0w + gi * 16) * ROWB;
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, (AVTP_LDS void *)(dst + i * 1024), 16, (int)voff[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, dst + i * 1024, 16, (int)voff[i], 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (AVTP_LDS void *)(dst + TB + i * 1024), 16, (int)voff[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, dst + TB + i * 1024, 16, (int)voff[i], 0, 0, 0);
     }
   };
 
@@ -256,7 +359,6 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
 #pragma unroll
   for (int i = 0; i < ND; ++i) O[i] = f32x16{};
   float m = -INFINITY, l = 0.f;  // this lane's share of the row's sum
-  const float cl2e = a.cl2e;
 
   // element e of a tile of this lane: key eoff(e) + 4 hi of the tile
   auto eoff = [](int e) __attribute__((always_inline)) { return 8 * (e >> 2) + (e & 3); };
@@ -430,193 +532,303 @@ __global__ __launch_bounds__(64 * WR * WK, (WK > 1 || D * sizeof(T) > 256 ? 1 : 
     }
   };
 
-  const int nstage = (kend - kbeg + KS - 1) / KS;
-  int ids = load_ids(kbeg);
-  issue(smA, kbeg, ids);
-  ids = load_ids(kbeg + KS);
-  auto step = [&](const char *buf, char *nxt, int st) __attribute__((always_inline)) {
-    const int ks = kbeg + st * KS;
-    wait_vmem();
-    if (WK == 1) __syncthreads();  // stage st is in LDS; every wave is done with the other buffer
-    if (st + 1 < nstage) {
-      issue(nxt, ks + KS, ids);
-      ids = load_ids(ks + 2 * KS);
-    }
-    // keys of this wave below the range's end, and the rows that see them
-    const int kb = ks + wk * TPW * kTile, stop = min(kend, wmax);
-    lptr kt = (lptr)(buf) + wk * TPW * kTile * ROWB, vt = kt + TB;
-    if (__builtin_expect(kb + TPW * kTile <= min(kend, wmin), 1) &&
-        __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
-      return;
+  const int nstage = kend > kbeg ? (kend - kbeg + KS - 1) / KS : 0;
+  if (WR > 1) __syncthreads();  // the waves are done with the tile before
+  if (nstage > 0) {
+    int ids = load_ids(kbeg);
+    issue(bufA, kbeg, ids);
+    ids = load_ids(kbeg + KS);
+    auto step = [&](AVTP_LDS const char *buf, AVTP_LDS char *nxt, int st) __attribute__((always_inline)) {
+      const int ks = kbeg + st * KS;
+      wait_vmem();
+      if (WR > 1) __syncthreads();  // stage st is in LDS; every wave is done with the other buffer
+      if (st + 1 < nstage) {
+        issue(nxt, ks + KS, ids);
+        ids = load_ids(ks + 2 * KS);
+      }
+      // keys below the range's end, and those that rows of this wave see
+      const int stop = min(kend, wmax);
+      lptr kt = buf, vt = kt + TB;
+      if (__builtin_expect(ks + KS <= min(kend, wmin), 1) &&
+          __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
+        return;
 #pragma unroll 1
-    for (int t = 0; t < TPW; ++t)
-      if (kb + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, kb + t * kTile);
-  };
-  for (int st = 0; st < nstage; st += 2) {
-    step(smA, smB, st);
-    if (st + 1 < nstage) step(smB, smA, st + 1);
+      for (int t = 0; t < TPW; ++t)
+        if (ks + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, ks + t * kTile);
+    };
+    for (int st = 0; st < nstage; st += 2) {
+      step(bufA, bufB, st);
+      if (st + 1 < nstage) step(bufB, bufA, st + 1);
+    }
   }
   l = half_sum(l);
 
-  // a finished row (or its part): values d .. d + 3, normalised
-  auto put = [&](long long at_out, long long at_row, int dd, f32x4 x) __attribute__((always_inline)) {
-    if (a.nsplit > 1) {
-      *reinterpret_cast<f32x4 *>(a.po + ((long long)split * a.N_q * a.Hq + at_row) * D + dd) = x;
-    } else if constexpr (F32) {
-      *reinterpret_cast<f32x4 *>(a.out + at_out + dd * 4) = x;
-    } else {
-      bf16x4 y;
+  // the finished rows, or the tile's part
+  if (!valid) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float ls = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // log2 of the row's sum
+  const long long pr = (long long)job.slot * BM + wave * kTile + col;
+  char *o = a.out + (job.s.q0 + tok) * a.out_tok + (long long)head * ROWB;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = (__bf16)x[i];
-      *reinterpret_cast<bf16x4 *>(a.out + at_out + dd * 2) = y;
+  for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int dd = 32 * dt + 8 * j + 4 * hi;
+      const f32x4 x = {O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv};
+      if (job.cut) *reinterpret_cast<f32x4 *>(a.po + pr * D + dd) = x;
+      else put4<T>(o, dd, x);
     }
-  };
-  // log2 of the row's sum
-  auto put_lse = [&](int t, int h, long long at_row, float x) __attribute__((always_inline)) {
-    if (a.nsplit > 1) a.pl[(long long)split * a.N_q * a.Hq + at_row] = x;
-    else if (a.lse) a.lse[(long long)h * a.N_q + sq.q0 + t] = x * kLn2;
-  };
-
-  if constexpr (WK == 1) {
-    if (!valid) return;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    const long long at_out = (sq.q0 + tok) * a.out_tok + (long long)head * ROWB;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        put(at_out, orow, 32 * dt + 8 * j + 4 * hi,
-            f32x4{O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv});
-    if (hi == 0) put_lse(tok, head, orow, l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l));
-  } else {
-    // Join the waves' parts: each leaves its O in LDS (in 16-byte chunks, XOR-ed
-    // with the row), its m and l beside it.
-    constexpr int OB = kTile * D * 4;  // bytes of a wave's O
-    static_assert(NW * OB <= 2 * TB, "the parts fit the first buffer");
-    __syncthreads();
-    char *mine = smA + wk * OB;
-#pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int ch = 8 * dt + 2 * j + hi;
-        *reinterpret_cast<f32x4 *>(mine + col * (D * 4) + ((ch ^ (col & (D / 4 - 1))) << 4)) =
-            f32x4{O[dt][4 * j], O[dt][4 * j + 1], O[dt][4 * j + 2], O[dt][4 * j + 3]};
-      }
-    if (hi == 0) {
-      ml_s[(wk * kTile + col) * 2] = m;
-      ml_s[(wk * kTile + col) * 2 + 1] = l;
-    }
-    __syncthreads();
-    const int rows = min(R - row0, kTile);
-    for (int i = tid; i < rows * (D / 4); i += NW * 64) {
-      const int r = i / (D / 4), ch = i % (D / 4);
-      float top = -INFINITY, tot = 0.f;
-#pragma unroll
-      for (int w = 0; w < WK; ++w) top = fmaxf(top, ml_s[(w * kTile + r) * 2]);
-      f32x4 x = f32x4{};
-#pragma unroll
-      for (int w = 0; w < WK; ++w) {
-        const float mw = ml_s[(w * kTile + r) * 2];
-        const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - top);
-        tot += ml_s[(w * kTile + r) * 2 + 1] * f;
-        const f32x4 y = *reinterpret_cast<const f32x4 *>(smA + w * OB + r * (D * 4) + ((ch ^ (r & (D / 4 - 1))) << 4));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x[j] += y[j] * f;
-      }
-      const float inv = tot == 0.f ? 0.f : 1.f / tot;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[j] *= inv;
-      const int t = (row0 + r) / a.G, h = g * a.G + (row0 + r - t * a.G);
-      const long long ar = (long long)(sq.q0 + t) * a.Hq + h;
-      put((sq.q0 + t) * a.out_tok + (long long)h * ROWB, ar, ch * 4, x);
-      if (ch == 0) put_lse(t, h, ar, tot == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(tot));
-    }
+  if (hi == 0) {
+    if (job.cut) a.pl[pr] = ls;
+    else if (a.lse) a.lse[(long long)head * a.N_q + job.s.q0 + tok] = ls * kLn2;
   }
 }
 
-// Joins the parts of the key ranges: a group of D / 4 threads per (token, head).
+// Few rows per sequence (decode steps): a block is one wave, a worker that takes
+// its share of the line of units.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void page_join_kernel(KArgs a) {
-  constexpr int TPR = D / 4;
-  const long long rows = (long long)a.N_q * a.Hq;
-  const long long r = (long long)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  const int ch = threadIdx.x % TPR;
-  const int t = (int)(r / a.Hq), h = (int)(r - (long long)t * a.Hq);
-  if (r >= rows || t < a.cu_q[0] || t >= a.cu_q[a.B]) return;
-  float top = -INFINITY;
-  for (int s = 0; s < a.nsplit; ++s) top = fmaxf(top, a.pl[s * rows + r]);
-  float tot = 0.f;
-  f32x4 x = f32x4{};
-  for (int s = 0; s < a.nsplit; ++s) {
-    const float ls = a.pl[s * rows + r];
-    if (ls == -INFINITY) continue;  // no key in this range: nothing was written
-    const float f = __builtin_amdgcn_exp2f(ls - top);
-    const f32x4 y = *reinterpret_cast<const f32x4 *>(a.po + (s * rows + r) * D + ch * 4);
-    tot += f;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] += y[j] * f;
+__global__ __launch_bounds__(64, (Shape<T, D, 1, 1>::kPerSimd)) void page_attn_few_kernel(KArgs a) {
+  using S_ = Shape<T, D, 1, 1>;
+  constexpr int BM = S_::BM, KS = S_::KS;
+  // two stage buffers as distinct objects, so the compiler can tell the one
+  // being read from the one in flight
+  __shared__ __attribute__((aligned(16))) char smA[2 * S_::TB];
+  __shared__ __attribute__((aligned(16))) char smB[2 * S_::TB];
+  const int worker = blockIdx.x;
+  Seq first;
+  const u64 units = seq_units<BM, KS>(a, 0, first);
+  u64 per = wave::sum(units);
+  for (int c0 = 64; c0 < a.B; c0 += 64) {
+    Seq x;
+    per += wave::sum(seq_units<BM, KS>(a, c0, x));
   }
-  const float inv = tot == 0.f ? 0.f : 1.f / tot;
-  char *o = a.out + t * a.out_tok + (long long)h * D * sizeof(T) + ch * 4 * sizeof(T);
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<f32x4 *>(o) = f32x4{x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv};
-  } else {
-    bf16x4 y;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) y[j] = (__bf16)(x[j] * inv);
-    *reinterpret_cast<bf16x4 *>(o) = y;
+  const u64 all = per * (unsigned)a.Hkv;
+  u64 share = (all + a.workers - 1) / a.workers;
+  if (share < (unsigned)a.least) share = a.least;
+  u64 w = share * worker;
+  const u64 wend = w + share < all ? w + share : all;
+  Cut c{};
+  if (w < wend) {
+    Place<BM, KS> at;
+    at.find(a, w, per, units, first);
+    for (;;) {
+      const int u1 = (u64)(at.U - at.u) <= wend - w ? at.U : at.u + (int)(wend - w);
+      Job job{at.g, at.b, at.t * BM, at.u * KS, min(tile_keys<BM>(a, at.s, at.t), u1 * KS),
+              2 * worker + (at.u > 0 ? 0 : 1), at.u > 0 || u1 < at.U, at.s};
+      attend<T, D, 1, 1>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
+      // (a worker's first part of a tile is the odd one of its slots; the
+      // workers behind it go on in their even ones)
+      if (at.u == 0 && job.cut)
+        c = {(int)((at.U - u1 + share - 1) / share), at.g, at.s.q0, at.s.n, job.row0, job.slot, 2 * (worker + 1), 2};
+      w += u1 - at.u;
+      if (w >= wend) break;
+      at.next(a);
+    }
   }
-  if (ch == 0 && a.lse)
-    a.lse[(long long)h * a.N_q + t] = tot == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(tot)) * kLn2;
+  if (threadIdx.x == 0) put_cut(a.meta, worker, c);
 }
 
-constexpr int kManyWaves = 4;                    // row waves of a block of many rows
-constexpr int kManyRows = kManyWaves * kTile;
+// Many rows per sequence (chunks of tokens): a block takes one tile of 128 rows
+// of one key head, or one of nsplit ranges of its keys where there are few
+// tiles.  The tiles of one sequence go together, key heads fastest, so that
+// an XCD (blocks equal mod 8) reads the same K and V at about the same time: in
+// the even line above, whose workers stand at different keys, four prompts of
+// 7,000-9,000 tokens took 2907 us, with blocks in step 2147.
+template <typename T, int D, int WR, int TPW>
+__global__ __launch_bounds__(64 * WR, (Shape<T, D, WR, TPW>::kPerSimd)) void page_attn_many_kernel(KArgs a) {
+  using S_ = Shape<T, D, WR, TPW>;
+  constexpr int BM = S_::BM, KS = S_::KS;
+  __shared__ __attribute__((aligned(16))) char smA[2 * S_::TB];
+  __shared__ __attribute__((aligned(16))) char smB[2 * S_::TB];
+  const int lane = threadIdx.x & 63;
+  const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
+  const int split = rest % a.nsplit, rank = rest / a.nsplit;
+  const int place = rank * a.Hkv + g;  // of the tile among all
+  int b = 0, tile = -1;
+  Seq s{};
+  if (a.B <= 64) {
+    // longest sequences first, the tiles that see most first: what is left at
+    // the end is small
+    const Seq mine = seq_of(a, min(lane, a.B - 1));
+    const int nt = lane < a.B ? tiles_of<BM>(a, mine) : 0;
+    int before = 0;
+    for (int j = 0; j < a.B; ++j) {
+      const int kv = __builtin_amdgcn_readlane(mine.L, j), n = __builtin_amdgcn_readlane(nt, j);
+      if (kv > mine.L || (kv == mine.L && j < lane)) before += n;
+    }
+    const u64 m = __ballot(before <= rank && rank < before + nt);
+    if (m != 0) {
+      b = __builtin_ctzll(m);
+      s = uniform(mine, b);
+      tile = __builtin_amdgcn_readlane(before + nt, b) - 1 - rank;
+    }
+  } else {
+    // Sequence b's tiles have the ranks from floor(q0 G / BM) + b on: the next
+    // sequence's start at least ceil(n G / BM) further, so that no sum over the
+    // sequences is needed.
+    auto start = [&](int x) __attribute__((always_inline)) {
+      return min(max(0, a.cu_q[x]), a.N_q) * a.G / BM + x;
+    };
+    int lo = 0;
+    for (int step = 1 << 12; step > 0; step >>= 6) {  // (B is 2^16 at most)
+      const int x = lo + lane * step;
+      const u64 m = __ballot(x < a.B && start(min(x, a.B - 1)) <= rank);
+      lo += max(0, __builtin_popcountll(m) - 1) * step;
+    }
+    b = lo;
+    s = uniform(seq_of(a, b), 0);
+    tile = rank - __builtin_amdgcn_readfirstlane(start(b));
+    if (tile >= tiles_of<BM>(a, s)) tile = -1;
+  }
+  Cut c{};
+  if (tile >= 0) {
+    const int keys = tile_keys<BM>(a, s, tile);
+    // whole stages, evenly; a range has `least` keys or more
+    const int stages = max(1, (keys + KS - 1) / KS);
+    const int ranges = min(a.nsplit, max(1, (keys + a.least - 1) / a.least)), each = (stages + ranges - 1) / ranges;
+    const int parts = (stages + each - 1) / each;
+    if (split >= parts) return;
+    const Job job{g, b, tile * BM, split * each * KS, min(keys, (split + 1) * each * KS), place * a.nsplit + split,
+                  parts > 1, s};
+    attend<T, D, WR, TPW>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
+    c = {parts - 1, g, s.q0, s.n, job.row0, job.slot, job.slot + 1, 1};
+  }
+  if (a.nsplit > 1 && split == 0 && threadIdx.x == 0) put_cut(a.meta, place, c);
+}
+
+// Joins the parts of the tiles that were cut: D / 4 threads per row, a block
+// for each 1024 / D rows of a tile.  Where a tile has fewer rows than that, the
+// groups of threads share out its parts instead.
+template <typename T, int D, int BM>
+__global__ __launch_bounds__(256) void page_join_kernel(KArgs a) {
+  constexpr int TPR = D / 4, GROUPS = 256 / TPR;
+  __shared__ f32x4 x_s[256];
+  __shared__ float m_s[GROUPS], l_s[GROUPS];
+  const Cut t = get_cut(a.meta, blockIdx.x / (BM / GROUPS));
+  const int r0 = (blockIdx.x % (BM / GROUPS)) * GROUPS;
+  const int rows = min(t.n * a.G - t.row0 - r0, GROUPS);
+  if (t.more == 0 || rows <= 0) return;
+  int wide = 1;  // rows side by side: a power of two
+  while (wide < rows) wide <<= 1;
+  const int ch = threadIdx.x % TPR, grp = threadIdx.x / TPR;
+  const int i = grp & (wide - 1), first = grp / wide, step = GROUPS / wide;
+  const int r = r0 + min(i, rows - 1);
+  auto part = [&](int s) __attribute__((always_inline)) {
+    return (long long)(s == 0 ? t.first : t.next + (s - 1) * t.step) * BM + r;
+  };
+  // a running reference: the parts are read once, four at a time
+  float top = -INFINITY, tot = 0.f;
+  f32x4 x = f32x4{};
+  for (int s = first; s <= t.more; s += 4 * step) {
+    float ls[4];
+    f32x4 y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const long long at = part(min(s + j * step, t.more));
+      ls[j] = s + j * step <= t.more ? a.pl[at] : -INFINITY;
+      y[j] = *reinterpret_cast<const f32x4 *>(a.po + at * D + ch * 4);
+    }
+    const float nm = fmaxf(top, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3])));
+    const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - nm);
+    top = nm;
+    tot *= f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] *= f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (ls[j] == -INFINITY) continue;  // nothing in this part (or there is none)
+      const float e = __builtin_amdgcn_exp2f(ls[j] - top);
+      tot += e;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] += y[j][k] * e;
+    }
+  }
+  if (step > 1) {
+    x_s[threadIdx.x] = x;
+    if (ch == 0) {
+      m_s[grp] = top;
+      l_s[grp] = tot;
+    }
+    __syncthreads();
+    if (first > 0) return;
+    for (int j = 0; j < step; ++j) top = fmaxf(top, m_s[i + j * wide]);
+    tot = 0.f;
+    x = f32x4{};
+    for (int j = 0; j < step; ++j) {
+      const float ms = m_s[i + j * wide], e = ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - top);
+      const f32x4 y = x_s[threadIdx.x + j * wide * TPR];
+      tot += l_s[i + j * wide] * e;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] += y[k] * e;
+    }
+  }
+  if (i >= rows) return;
+  const float inv = tot == 0.f ? 0.f : 1.f / tot;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) x[k] *= inv;
+  const int tok = (t.row0 + r) / a.G, head = t.g * a.G + (t.row0 + r - tok * a.G);
+  put4<T>(a.out + (t.q0 + tok) * a.out_tok + (long long)head * D * (int)sizeof(T), ch * 4, x);
+  if (ch == 0 && a.lse)
+    a.lse[(long long)head * a.N_q + t.q0 + tok] = tot == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(tot)) * kLn2;
+}
+
+constexpr int kManyWaves = 4;
+// 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
+constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
 }  // namespace
 
 PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len) {
   PageAttnPlan L{};
-  // (a longer sequence still runs: the last range takes the rest)
-  max_kv_len = max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
-  const int64_t G = Hq / P.Hkv, rows = N_q * G;
+  const int row_bytes = P.d * (P.dtype == AVTP_FP32 ? 4 : 2);
+  // (longer sequences run all the same)
+  max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
+  const int64_t rows = N_q * (Hq / P.Hkv);
   L.few = rows <= (int64_t)B * kTile;
-  const int bm = L.few ? kTile : kManyRows;
-  const int64_t tiles = rows / bm + B;
-  L.tiles = (int)tiles;
-  // about 512 blocks, of 512 keys or more
-  const int64_t blocks = tiles * P.Hkv;
-  const int64_t most = (max_kv_len + 511) / 512;
-  int64_t ns = 512 / (blocks < 1 ? 1 : blocks);
-  ns = ns < 1 ? 1 : (ns > most ? (most < 1 ? 1 : most) : ns);
-  int64_t chunk = (max_kv_len + ns - 1) / ns;
-  chunk = (chunk + 127) / 128 * 128;
-  if (chunk < 128) chunk = 128;
-  L.nsplit = (int)ns;
-  L.chunk = (int)chunk;
-  if (L.nsplit > 1) {
-    const size_t r = (size_t)N_q * Hq;
-    L.off_lse = (r * L.nsplit * P.d * 4 + 255) / 256 * 256;
-    L.bytes = L.off_lse + r * L.nsplit * 4;
+  const int bm = L.few ? kTile : kManyWaves * kTile;
+  // (at most; many of more than 64 sequences: the ranks the kernel gives them)
+  const int64_t tiles = (rows / bm + (L.few && N_q < B ? N_q : B)) * P.Hkv;
+  int64_t slots;
+  if (L.few) {
+    // four workers per CU, what their LDS holds; fewer where there is less
+    // work than `least` units (a tile's 32 keys) for each
+    const int64_t most = row_bytes > 256 ? 512 : row_bytes > 128 ? 1024 : 2048;
+    L.least = 1;
+    const int64_t need = (tiles * ((max_kv_len + kTile - 1) / kTile) + L.least - 1) / L.least;
+    L.blocks = need < most ? need : most;
+    L.cuts = (int)L.blocks;
+    slots = 2 * L.blocks;
+  } else {
+    // two blocks per CU (one of fp32 rows of 512 bytes), of 256 keys or more (64
+    // in fp32, whose products take 16 times as long)
+    const int64_t want = row_bytes > 256 ? 256 : 512;
+    L.least = P.dtype == AVTP_FP32 ? 64 : 256;
+    const int64_t most = (max_kv_len + L.least - 1) / L.least;
+    const int64_t ns = tiles < 1 ? 1 : want / tiles;
+    L.nsplit = (int)(ns < 1 ? 1 : ns < most ? ns : most);
+    L.blocks = tiles * L.nsplit;
+    L.cuts = L.nsplit > 1 ? (int)tiles : 0;
+    slots = L.nsplit > 1 ? L.blocks : 0;
+  }
+  if (N_q > 0 && L.cuts > 0) {
+    L.off_lse = (size_t)slots * bm * P.d * 4;
+    L.off_meta = L.off_lse + (size_t)slots * bm * 4;
+    L.bytes = L.off_meta + (size_t)L.cuts * 32;
   }
   return L;
 }
 
 template <typename T, int D>
 static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) {
-  const dim3 grid((unsigned)((long long)L.tiles * k.Hkv * L.nsplit));
-  if (L.few) {
-    constexpr int WK = sizeof(T) == 4 && D == 128 ? 2 : 4;
-    hipLaunchKernelGGL((page_attn_kernel<T, D, 1, WK, 1>), grid, dim3(64 * WK), 0, st, k);
-  } else {
-    constexpr int TPW = sizeof(T) == 4 && D == 128 ? 1 : 2;
-    hipLaunchKernelGGL((page_attn_kernel<T, D, kManyWaves, 1, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);
-  }
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || L.nsplit == 1) return e;
-  const long long rows = (long long)k.N_q * k.Hq, per = 256 / (D / 4);
-  hipLaunchKernelGGL((page_join_kernel<T, D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, st, k);
+  constexpr int TPW = many_tiles(D * (int)sizeof(T));
+  const dim3 grid((unsigned)L.blocks);
+  if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D>), grid, dim3(64), 0, st, k);
+  else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || L.cuts == 0) return e;
+  const unsigned per = (L.few ? 1 : kManyWaves) * kTile * D / 1024;  // blocks per tile
+  if (L.few) hipLaunchKernelGGL((page_join_kernel<T, D, kTile>), dim3(L.cuts * per), dim3(256), 0, st, k);
+  else hipLaunchKernelGGL((page_join_kernel<T, D, kManyWaves * kTile>), dim3(L.cuts * per), dim3(256), 0, st, k);
   return hipGetLastError();
 }
 
@@ -634,6 +846,7 @@ hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const Page
   k.lse = A.lse;
   k.po = (float *)ws;
   k.pl = (float *)(ws + L.off_lse);
+  k.meta = (int4 *)(ws + L.off_meta);
   k.cu_q = A.cu_q;
   k.kv_len = A.kv_len;
   k.table = A.table;
@@ -646,12 +859,11 @@ hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const Page
   k.max_pages = A.max_pages;
   k.n_pages = P.n_pages;
   k.page_shift = __builtin_ctz((unsigned)P.page_size);
+  k.workers = (int)L.blocks;
   k.nsplit = L.nsplit;
-  k.chunk = L.chunk;
+  k.least = L.least;
   k.cl2e = A.scale * kLog2e;
-  if (P.dtype == AVTP_FP32) {
-    return P.d == 64 ? launch<float, 64>(st, L, k) : launch<float, 128>(st, L, k);
-  }
+  if (P.dtype == AVTP_FP32) return P.d == 64 ? launch<float, 64>(st, L, k) : launch<float, 128>(st, L, k);
   return P.d == 64 ? launch<__bf16, 64>(st, L, k) : launch<__bf16, 128>(st, L, k);
 }
 
