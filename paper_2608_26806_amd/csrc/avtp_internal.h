@@ -143,7 +143,8 @@ hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void
 // Attention over the pages: its launch, from host-known sizes only (so the
 // workspace size and the launch always agree).
 struct PageAttnPlan {
-  bool few;        // few rows per sequence: tiles of 32 rows, else of 128
+  bool few;        // few rows per sequence: one wave has them all
+  int tile;        // rows of a tile: 16 or 32 (few), 128
   int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
   int nsplit;      // many: key ranges per tile
   int least;       // few: units (32 keys of a tile) per worker, many: keys per range, at least

@@ -42,7 +42,7 @@ typedef __amdgpu_buffer_rsrc_t Rsrc;
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kTile = 32;  // query rows and keys of an MFMA tile
+constexpr int kTile = 32;  // keys of a tile
 // A row's exponentials refer to the largest logit m of some earlier tile, not
 // always of all: only when their sum over a tile leaves this range is m raised
 // (and the sum and output so far scaled).  fp32 sums, and products with bf16 or
@@ -55,8 +55,6 @@ struct Geo {
   static constexpr int ROWB = D * (int)sizeof(T);  // bytes of a head row
   static constexpr int NCH = ROWB / 16;            // its 16-byte chunks
   static constexpr int RPL = 64 / NCH;             // rows of a wave's load
-  static constexpr int NS = D * (int)sizeof(T) / 32;  // K fragments per key (16 bytes per lane half)
-  static constexpr int ND = D / 32;                // output tiles of 32 values
   // Chunk order inside an LDS row, XOR-ed with the row: 16 consecutive rows of
   // one chunk (a K fragment) lie in 16 different places of the 64 banks, and so
   // do the four 64-byte pieces of consecutive rows that a transposing read of
@@ -103,22 +101,51 @@ __device__ inline Rsrc make_rsrc(const char *p, int bytes) {
                                            0x00027000);
 }
 
+// wait for this wave's outstanding loads, direct-to-LDS ones included
 __device__ inline void wait_vmem() {
   __builtin_amdgcn_s_waitcnt(0xF70);
   asm volatile("" ::: "memory");
 }
 
-// of both lane halves: combine(x, the value 32 lanes away)
-__device__ inline float half_max(float x) {
-  const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x),
-                                                  false, false);
-  return fmaxf(__builtin_bit_cast(float, (unsigned)p[0]), __builtin_bit_cast(float, (unsigned)p[1]));
+// Over the lanes that hold the same row, 64 / M of them M lanes apart.
+template <int M, typename F>
+__device__ inline float over_row(float x, F f) {
+  auto both = [&](auto p) __attribute__((always_inline)) {
+    return f(__builtin_bit_cast(float, (unsigned)p[0]), __builtin_bit_cast(float, (unsigned)p[1]));
+  };
+  if (M == 16) {
+    const unsigned u = __builtin_bit_cast(unsigned, x);
+    x = both(__builtin_amdgcn_permlane16_swap(u, u, false, false));
+  }
+  const unsigned u = __builtin_bit_cast(unsigned, x);
+  return both(__builtin_amdgcn_permlane32_swap(u, u, false, false));
 }
-__device__ inline float half_sum(float x) {
-  const auto p = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(unsigned, x), __builtin_bit_cast(unsigned, x),
-                                                  false, false);
-  return __builtin_bit_cast(float, (unsigned)p[0]) + __builtin_bit_cast(float, (unsigned)p[1]);
-}
+
+// The MFMA of M rows and columns.  A lane holds column lane mod M; of the M rows
+// it holds those with (row / 4) mod (64 / M) = lane / M, and of a product's
+// inner index the share number lane / M.
+template <int M>
+struct Mma;
+template <>
+struct Mma<32> {
+  typedef f32x16 acc;
+  static __device__ inline acc run(bf16x8 a, bf16x8 b, acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ inline acc run(float a, float b, acc c) {
+    return __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, c, 0, 0, 0);
+  }
+};
+template <>
+struct Mma<16> {
+  typedef f32x4 acc;
+  static __device__ inline acc run(bf16x8 a, bf16x8 b, acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ inline acc run(float a, float b, acc c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+  }
+};
 
 // The work.  A row tile is BM rows (token, head of the group) of one sequence
 // and key head; a unit is one stage of KS keys of a tile, and a tile has the
@@ -273,43 +300,55 @@ struct Job {
   Seq s;
 };
 
-// WR waves of 32 rows each share the stages of TPW tiles of 32 keys.
-template <typename T, int D, int WR, int TPW>
+// WR waves of M rows each share the stages of TPW tiles of 32 keys.
+template <typename T, int D, int M, int WR, int TPW>
 struct Shape {
   using G_ = Geo<T, D>;
-  static constexpr int BM = WR * kTile;
+  static constexpr int BM = WR * M;
   static constexpr int KS = TPW * kTile;           // keys per stage
   static constexpr int RW = KS / WR;               // of them, rows a wave loads
   static constexpr int GR = RW < 16 ? RW : 16;     // rows of one page group
   static constexpr int NG = RW / GR, LPG = GR / G_::RPL;
   static_assert(RW % G_::RPL == 0 && GR % G_::RPL == 0, "whole loads");
   static constexpr int TB = KS * G_::ROWB;         // bytes of one tensor's stage
-  // two waves per SIMD, one where the registers of an fp32 tile leave room for one
-  static constexpr int kPerSimd = G_::ROWB > 256 ? 1 : 2;
+  // Blocks per CU, with two stage buffers each.  One-wave workers: one wave per
+  // SIMD (two where a stage is small) keeps 64 KB in flight.  More of them, or a
+  // third buffer, is slower: a decode step of two requests of 128,000 tokens takes
+  // 171 us with four workers of two buffers, 204 with five, 183 with three of
+  // three.  Chunks: two blocks, of an fp32 tile of 512-byte rows one, by its registers.
+  static constexpr int kPerCu = WR > 1 ? (G_::ROWB > 256 ? 1 : 2) : 128 * 1024 / (4 * TB);
+  static constexpr int kPerSimd = (kPerCu * WR + 3) / 4;
 };
 
-template <typename T, int D, int WR, int TPW>
+template <typename T, int D, int M, int WR, int TPW>
 __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, const Job &job, AVTP_LDS char *bufA,
                                                              AVTP_LDS char *bufB) {
   using G_ = Geo<T, D>;
-  using S_ = Shape<T, D, WR, TPW>;
+  using S_ = Shape<T, D, M, WR, TPW>;
+  using M_ = Mma<M>;
   constexpr bool F32 = G_::F32;
   constexpr int BM = S_::BM, KS = S_::KS, RW = S_::RW, GR = S_::GR, NG = S_::NG, LPG = S_::LPG, TB = S_::TB;
-  constexpr int ROWB = G_::ROWB, NCH = G_::NCH, RPL = G_::RPL, NS = G_::NS, ND = G_::ND;
+  constexpr int ROWB = G_::ROWB, NCH = G_::NCH, RPL = G_::RPL;
+  constexpr int NGR = 64 / M;        // lane groups: lanes of one row
+  constexpr int NK = kTile / M;      // S tiles of M keys
+  constexpr int NS = NCH / NGR;      // K fragments per key: chunks of 16 bytes, one a group
+  constexpr int ND = D / M;          // output tiles of M values
+  constexpr int AE = M * M / 64;     // a lane's elements of an M x M tile
+  constexpr int NE = NK * AE;        // and of a tile's logits
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = WR > 1 ? __builtin_amdgcn_readfirstlane(tid >> 6) : 0;
-  const int hi = lane >> 5, col = lane & 31;
+  const int grp = lane / M, col = lane % M;
   const float cl2e = a.cl2e;
   const int pmask = (1 << a.page_shift) - 1;
   const int g = job.g, b = job.b, L = job.s.L, row0 = job.row0, kbeg = job.kbeg, kend = job.kend;
   const int R = job.s.n * a.G;
   if (L < job.s.kv && a.status && tid == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
   // row r of the sequence: token r / G, which sees kv - n + token + 1 keys
-  const int wrow = row0 + wave * kTile;
+  const int wrow = row0 + wave * M;
   const int row = min(wrow + col, R - 1), tok = row / a.G, head = g * a.G + (row - tok * a.G);
   const int lim = min(L, job.s.kv - job.s.n + tok + 1);
   const bool valid = wrow + col < R;
-  const int wmin = __builtin_amdgcn_readlane(lim, 0), wmax = __builtin_amdgcn_readlane(lim, 31);
+  const int wmin = __builtin_amdgcn_readlane(lim, 0), wmax = __builtin_amdgcn_readlane(lim, M - 1);
 
   // where this lane's loads of a 16-row group come from
   uint32_t voff[LPG];
@@ -323,9 +362,9 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   // query rows, the second operand of S^T
   u32x4 qf[NS];
   {
-    const char *p = a.q + (job.s.q0 + tok) * a.q_tok + (long long)head * ROWB + hi * 16;
+    const char *p = a.q + (job.s.q0 + tok) * a.q_tok + (long long)head * ROWB + grp * 16;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(p + s * 32);
+    for (int s = 0; s < NS; ++s) qf[s] = *reinterpret_cast<const u32x4 *>(p + s * NGR * 16);
   }
 
   const int32_t *trow = a.table + (long long)b * a.max_pages;
@@ -335,6 +374,9 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     const int key = min(ks + r0w + (lane & (NG - 1)) * 16, L - 1);
     return trow[key >> a.page_shift];
   };
+  // Decode steps read K and V once: non-temporal (64 requests' step 206 -> 194 us;
+  // chunks read them again, from the L2).
+  constexpr int kAux = WR == 1 ? 2 : 0;
   auto issue = [&](AVTP_LDS char *buf, int ks, int ids) __attribute__((always_inline)) {
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
@@ -348,49 +390,53 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
       AVTP_LDS char *dst = buf + (r0w + gi * 16) * ROWB;
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, dst + i * 1024, 16, (int)voff[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rk, dst + i * 1024, 16, (int)voff[i], 0, 0, kAux);
 #pragma unroll
       for (int i = 0; i < LPG; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, dst + TB + i * 1024, 16, (int)voff[i], 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, dst + TB + i * 1024, 16, (int)voff[i], 0, 0, kAux);
     }
   };
 
-  f32x16 O[ND];
+  typename M_::acc O[ND];
 #pragma unroll
-  for (int i = 0; i < ND; ++i) O[i] = f32x16{};
+  for (int i = 0; i < ND; ++i) O[i] = typename M_::acc{};
   float m = -INFINITY, l = 0.f;  // this lane's share of the row's sum
 
-  // element e of a tile of this lane: key eoff(e) + 4 hi of the tile
-  auto eoff = [](int e) __attribute__((always_inline)) { return 8 * (e >> 2) + (e & 3); };
+  // element e of this lane: key (of a tile's logits) or value (of an output
+  // tile) eoff(e) + 4 grp
+  auto eoff = [](int e) __attribute__((always_inline)) { return 4 * NGR * (e >> 2) + (e & 3); };
 
   // LDS addresses of a tile's operands: the lane's base, XOR-ed with the chunk,
   // plus rows that fit the instruction's offset.
-  // K: row col, fragment s
+  // K: row kk M + col, fragment s
   typedef AVTP_LDS const char *lptr;
-  const uint32_t kbase = (uint32_t)(col * ROWB + ((hi ^ G_::swz(col)) << 4));
-  auto kaddr = [&](lptr kt, int s) __attribute__((always_inline)) { return kt + (kbase ^ (uint32_t)(s << 5)); };
+  const uint32_t kbase = (uint32_t)(col * ROWB + ((grp ^ G_::swz(col)) << 4));
+  auto kaddr = [&](lptr kt, int kk, int s) __attribute__((always_inline)) {
+    return kt + (kbase ^ (uint32_t)(s * NGR << 4)) + kk * M * ROWB;
+  };
   // V, bf16: the transposing read hands lane i of 16 the value i of four rows of
   // 16 values whose addresses the lanes give (lane i: four values of row i / 4),
-  // here 32 dt + col of the four keys 16 c + 8 j + 4 hi + .. that belong to the
-  // lane's probabilities 8 c + 4 j + ..
-  const int ti = lane & 15, tq = (lane >> 4) & 1;
-  const int vrow = F32 ? 4 * hi : 4 * hi + (ti >> 2);
+  // here M dt + col of the four keys eoff(8 c + 4 j) + 4 grp + .. that belong to
+  // the lane's probabilities 8 c + 4 j + ..
+  const int ti = lane & 15, tq = (lane >> 4) & (M / 16 - 1);
+  const int vrow = F32 ? 4 * grp : 4 * grp + (ti >> 2);
   const uint32_t vbase = F32 ? (uint32_t)(vrow * ROWB + (((col >> 2) ^ G_::swz(vrow)) << 4) + (col & 3) * 4)
                              : (uint32_t)(vrow * ROWB + (((2 * tq + ((ti & 3) >> 1)) ^ G_::swz(vrow)) << 4) + (ti & 1) * 8);
   auto vfrag = [&](lptr vt, int c, int dt) __attribute__((always_inline)) {
     bf16x8 f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
-      const uint32_t o = (vbase ^ (uint32_t)(dt << 6 | (G_::swz(8 * j) << 4))) + (uint32_t)((16 * c + 8 * j) * ROWB);
+      const int r = eoff(8 * c + 4 * j);
+      const uint32_t o = (vbase ^ (uint32_t)(((dt * M / 8) ^ G_::swz(r)) << 4)) + (uint32_t)(r * ROWB);
       const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((AVTP_LDS bf16x4 *)(vt + o));
 #pragma unroll
       for (int i = 0; i < 4; ++i) f[4 * j + i] = x[i];
     }
     return f;
   };
-  // fp32: value 32 dt + col of key eoff(e) + 4 hi
+  // fp32: value M dt + col of key eoff(e) + 4 grp
   auto velem = [&](lptr vt, int e, int dt) __attribute__((always_inline)) {
-    const uint32_t o = (vbase ^ (uint32_t)(((8 * dt) ^ G_::swz(eoff(e))) << 4)) + (uint32_t)(eoff(e) * ROWB);
+    const uint32_t o = (vbase ^ (uint32_t)(((dt * M / 4) ^ G_::swz(eoff(e))) << 4)) + (uint32_t)(eoff(e) * ROWB);
     return *reinterpret_cast<AVTP_LDS const float *>(vt + o);
   };
 
@@ -417,8 +463,8 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const int dd = 32 * dt + eoff(e) + 4 * hi;  // this lane's value of the output
+        for (int e = 0; e < AE; ++e) {
+          const int dd = M * dt + eoff(e) + 4 * grp;  // this lane's value of the output
           const int ch = dd * (int)sizeof(T) / 16, by = dd * (int)sizeof(T) % 16;
           const float x =
               (float)*reinterpret_cast<AVTP_LDS const T *>(vt + r * ROWB + ((ch ^ G_::swz(r)) << 4) + by);
@@ -430,33 +476,40 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   };
 
   // S^T of the 32 keys at kt
+  struct Logits {
+    typename M_::acc x[NK];
+    __device__ inline float get(int e) const { return x[e / AE][e % AE]; }
+  };
   auto logits = [&](lptr kt) __attribute__((always_inline)) {
-    f32x16 S = f32x16{};
+    Logits S;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      if constexpr (F32) {
-        const f32x4 kf = *reinterpret_cast<AVTP_LDS const f32x4 *>(kaddr(kt, s)), qv = __builtin_bit_cast(f32x4, qf[s]);
+    for (int kk = 0; kk < NK; ++kk) {
+      S.x[kk] = typename M_::acc{};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[i], qv[i], S, 0, 0, 0);
-      } else {
-        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<AVTP_LDS const bf16x8 *>(kaddr(kt, s)),
-                                                    __builtin_bit_cast(bf16x8, qf[s]), S, 0, 0, 0);
+      for (int s = 0; s < NS; ++s) {
+        if constexpr (F32) {
+          const f32x4 kf = *reinterpret_cast<AVTP_LDS const f32x4 *>(kaddr(kt, kk, s)), qv = __builtin_bit_cast(f32x4, qf[s]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S.x[kk] = M_::run(kf[i], qv[i], S.x[kk]);
+        } else {
+          S.x[kk] = M_::run(*reinterpret_cast<AVTP_LDS const bf16x8 *>(kaddr(kt, kk, s)),
+                            __builtin_bit_cast(bf16x8, qf[s]), S.x[kk]);
+        }
       }
     }
     return S;
   };
   // p = 2^(c S - m), as the second product takes them, and their sum
-  struct Bf {
-    bf16x8 x[2];
+  struct Probs {
+    std::conditional_t<F32, float, bf16x8> x[F32 ? NE : NE / 8];
   };
-  typedef std::conditional_t<F32, f32x16, Bf> Probs;
-  auto probs = [&](const f32x16 &S, Probs &p, float ref) __attribute__((always_inline)) {
+  auto probs = [&](const Logits &S, Probs &p, float ref) __attribute__((always_inline)) {
     float sum[2];
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float x = __builtin_amdgcn_exp2f(S[e] * cl2e - ref);
+    for (int e = 0; e < NE; ++e) {
+      const float x = __builtin_amdgcn_exp2f(S.get(e) * cl2e - ref);
       sum[e & 1] = e < 2 ? x : sum[e & 1] + x;
-      if constexpr (F32) p[e] = x;
+      if constexpr (F32) p.x[e] = x;
       else p.x[e >> 3][e & 7] = (__bf16)x;
     }
     return sum[0] + sum[1];
@@ -465,17 +518,17 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   auto weigh = [&](lptr vt, const Probs &p, bool clean) __attribute__((always_inline)) {
     if constexpr (F32) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
+      for (int e = 0; e < NE; ++e) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
           float x = velem(vt, e, dt);
           if (clean) x = __builtin_fabsf(x) < INFINITY ? x : 0.f;
-          O[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[e], O[dt], 0, 0, 0);
+          O[dt] = M_::run(x, p.x[e], O[dt]);
         }
       }
     } else {
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
+      for (int c = 0; c < NE / 8; ++c) {
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
           bf16x8 f = vfrag(vt, c, dt);
@@ -483,7 +536,7 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 #pragma unroll
             for (int i = 0; i < 8; ++i) f[i] = __builtin_fabsf((float)f[i]) < INFINITY ? f[i] : (__bf16)0.f;
           }
-          O[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f, p.x[c], O[dt], 0, 0, 0);
+          O[dt] = M_::run(f, p.x[c], O[dt]);
         }
       }
     }
@@ -492,7 +545,7 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   // a row's sum left its range, or has no reference yet; `part` takes them.
   auto whole = [&](lptr kt, lptr vt, auto n_tag) __attribute__((always_inline)) {
     constexpr int N = decltype(n_tag)::value;
-    f32x16 S[N];
+    Logits S[N];
     Probs p[N];
     float tot = 0.f;
 #pragma unroll
@@ -508,21 +561,23 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   // A tile of keys from kb on, of which some rows may see a part or nothing, and
   // whose largest logit becomes the row's reference if it is larger.
   auto part = [&](lptr kt, lptr vt, int kb) __attribute__((always_inline)) {
-    f32x16 S = logits(kt);
+    Logits S = logits(kt);
     Probs p;
+    float top = -INFINITY;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) S[e] = kb + 4 * hi + eoff(e) < lim ? S[e] : -INFINITY;
-    float top = S[0];
-#pragma unroll
-    for (int e = 1; e < 16; ++e) top = fmaxf(top, S[e]);
-    const float nm = fmaxf(m, half_max(top) * cl2e);
+    for (int e = 0; e < NE; ++e) {
+      float &x = reinterpret_cast<float *>(&S)[e];
+      x = kb + 4 * grp + eoff(e) < lim ? x : -INFINITY;
+      top = fmaxf(top, x);
+    }
+    const float nm = fmaxf(m, over_row<M>(top, [](float x, float y) { return fmaxf(x, y); }) * cl2e);
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
     m = nm;
     l *= f;
 #pragma unroll
     for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) O[dt][e] *= f;
+      for (int e = 0; e < AE; ++e) O[dt][e] *= f;
     l += probs(S, p, m == -INFINITY ? 0.f : m);  // (no key seen so far: every term is 0)
     if (__builtin_expect(tile_not_finite(vt), 0)) {
       add_not_finite(vt, kb);
@@ -534,11 +589,22 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 
   const int nstage = kend > kbeg ? (kend - kbeg + KS - 1) / KS : 0;
   if (WR > 1) __syncthreads();  // the waves are done with the tile before
+  auto work = [&](lptr kt, int ks) __attribute__((always_inline)) {
+    const lptr vt = kt + TB;
+    if (__builtin_expect(ks + KS <= min(kend, wmin), 1) &&
+        __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
+      return;
+    // keys below the range's end, and those that rows of this wave see
+    const int stop = min(kend, wmax);
+#pragma unroll 1
+    for (int t = 0; t < TPW; ++t)
+      if (ks + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, ks + t * kTile);
+  };
   if (nstage > 0) {
     int ids = load_ids(kbeg);
     issue(bufA, kbeg, ids);
     ids = load_ids(kbeg + KS);
-    auto step = [&](AVTP_LDS const char *buf, AVTP_LDS char *nxt, int st) __attribute__((always_inline)) {
+    auto step = [&](lptr buf, AVTP_LDS char *nxt, int st) __attribute__((always_inline)) {
       const int ks = kbeg + st * KS;
       wait_vmem();
       if (WR > 1) __syncthreads();  // stage st is in LDS; every wave is done with the other buffer
@@ -546,39 +612,31 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
         issue(nxt, ks + KS, ids);
         ids = load_ids(ks + 2 * KS);
       }
-      // keys below the range's end, and those that rows of this wave see
-      const int stop = min(kend, wmax);
-      lptr kt = buf, vt = kt + TB;
-      if (__builtin_expect(ks + KS <= min(kend, wmin), 1) &&
-          __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
-        return;
-#pragma unroll 1
-      for (int t = 0; t < TPW; ++t)
-        if (ks + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, ks + t * kTile);
+      work(buf, ks);
     };
     for (int st = 0; st < nstage; st += 2) {
       step(bufA, bufB, st);
       if (st + 1 < nstage) step(bufB, bufA, st + 1);
     }
   }
-  l = half_sum(l);
+  l = over_row<M>(l, [](float x, float y) { return x + y; });
 
   // the finished rows, or the tile's part
   if (!valid) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float ls = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // log2 of the row's sum
-  const long long pr = (long long)job.slot * BM + wave * kTile + col;
+  const long long pr = (long long)job.slot * BM + wave * M + col;
   char *o = a.out + (job.s.q0 + tok) * a.out_tok + (long long)head * ROWB;
 #pragma unroll
   for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int dd = 32 * dt + 8 * j + 4 * hi;
+    for (int j = 0; j < AE / 4; ++j) {
+      const int dd = M * dt + eoff(4 * j) + 4 * grp;
       const f32x4 x = {O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv};
       if (job.cut) *reinterpret_cast<f32x4 *>(a.po + pr * D + dd) = x;
       else put4<T>(o, dd, x);
     }
-  if (hi == 0) {
+  if (grp == 0) {
     if (job.cut) a.pl[pr] = ls;
     else if (a.lse) a.lse[(long long)head * a.N_q + job.s.q0 + tok] = ls * kLn2;
   }
@@ -586,9 +644,9 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 
 // Few rows per sequence (decode steps): a block is one wave, a worker that takes
 // its share of the line of units.
-template <typename T, int D>
-__global__ __launch_bounds__(64, (Shape<T, D, 1, 1>::kPerSimd)) void page_attn_few_kernel(KArgs a) {
-  using S_ = Shape<T, D, 1, 1>;
+template <typename T, int D, int M>
+__global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_attn_few_kernel(KArgs a) {
+  using S_ = Shape<T, D, M, 1, 1>;
   constexpr int BM = S_::BM, KS = S_::KS;
   // two stage buffers as distinct objects, so the compiler can tell the one
   // being read from the one in flight
@@ -615,7 +673,7 @@ __global__ __launch_bounds__(64, (Shape<T, D, 1, 1>::kPerSimd)) void page_attn_f
       const int u1 = (u64)(at.U - at.u) <= wend - w ? at.U : at.u + (int)(wend - w);
       Job job{at.g, at.b, at.t * BM, at.u * KS, min(tile_keys<BM>(a, at.s, at.t), u1 * KS),
               2 * worker + (at.u > 0 ? 0 : 1), at.u > 0 || u1 < at.U, at.s};
-      attend<T, D, 1, 1>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
+      attend<T, D, M, 1, 1>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
       // (a worker's first part of a tile is the odd one of its slots; the
       // workers behind it go on in their even ones)
       if (at.u == 0 && job.cut)
@@ -635,8 +693,8 @@ __global__ __launch_bounds__(64, (Shape<T, D, 1, 1>::kPerSimd)) void page_attn_f
 // the even line above, whose workers stand at different keys, four prompts of
 // 7,000-9,000 tokens took 2907 us, with blocks in step 2147.
 template <typename T, int D, int WR, int TPW>
-__global__ __launch_bounds__(64 * WR, (Shape<T, D, WR, TPW>::kPerSimd)) void page_attn_many_kernel(KArgs a) {
-  using S_ = Shape<T, D, WR, TPW>;
+__global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void page_attn_many_kernel(KArgs a) {
+  using S_ = Shape<T, D, 32, WR, TPW>;
   constexpr int BM = S_::BM, KS = S_::KS;
   __shared__ __attribute__((aligned(16))) char smA[2 * S_::TB];
   __shared__ __attribute__((aligned(16))) char smB[2 * S_::TB];
@@ -690,7 +748,7 @@ __global__ __launch_bounds__(64 * WR, (Shape<T, D, WR, TPW>::kPerSimd)) void pag
     if (split >= parts) return;
     const Job job{g, b, tile * BM, split * each * KS, min(keys, (split + 1) * each * KS), place * a.nsplit + split,
                   parts > 1, s};
-    attend<T, D, WR, TPW>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
+    attend<T, D, 32, WR, TPW>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
     c = {parts - 1, g, s.q0, s.n, job.row0, job.slot, job.slot + 1, 1};
   }
   if (a.nsplit > 1 && split == 0 && threadIdx.x == 0) put_cut(a.meta, place, c);
@@ -784,15 +842,21 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // (longer sequences run all the same)
   max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
   const int64_t rows = N_q * (Hq / P.Hkv);
-  L.few = rows <= (int64_t)B * kTile;
-  const int bm = L.few ? kTile : kManyWaves * kTile;
+  // one wave of 16 or 32 rows for a sequence, or blocks of 128
+  L.few = rows <= (int64_t)B * 32;
+  const int bm = L.tile = rows <= (int64_t)B * 16 ? 16 : L.few ? 32 : kManyWaves * 32;
   // (at most; many of more than 64 sequences: the ranks the kernel gives them)
   const int64_t tiles = (rows / bm + (L.few && N_q < B ? N_q : B)) * P.Hkv;
   int64_t slots;
   if (L.few) {
-    // four workers per CU, what their LDS holds; fewer where there is less
-    // work than `least` units (a tile's 32 keys) for each
-    const int64_t most = row_bytes > 256 ? 512 : row_bytes > 128 ? 1024 : 2048;
+    // as many workers as the CUs' LDS holds; fewer where there is less work than
+    // `least` units (a tile's 32 keys) for each
+    auto per_cu = [&](auto m_tag) {
+      constexpr int M = decltype(m_tag)::value;
+      if (P.dtype == AVTP_FP32) return P.d == 64 ? Shape<float, 64, M, 1, 1>::kPerCu : Shape<float, 128, M, 1, 1>::kPerCu;
+      return P.d == 64 ? Shape<__bf16, 64, M, 1, 1>::kPerCu : Shape<__bf16, 128, M, 1, 1>::kPerCu;
+    };
+    const int64_t most = 256 * (bm == 16 ? per_cu(std::integral_constant<int, 16>{}) : per_cu(std::integral_constant<int, 32>{}));
     L.least = 1;
     const int64_t need = (tiles * ((max_kv_len + kTile - 1) / kTile) + L.least - 1) / L.least;
     L.blocks = need < most ? need : most;
@@ -822,13 +886,15 @@ template <typename T, int D>
 static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) {
   constexpr int TPW = many_tiles(D * (int)sizeof(T));
   const dim3 grid((unsigned)L.blocks);
-  if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D>), grid, dim3(64), 0, st, k);
+  if (L.tile == 16) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 16>), grid, dim3(64), 0, st, k);
+  else if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 32>), grid, dim3(64), 0, st, k);
   else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || L.cuts == 0) return e;
-  const unsigned per = (L.few ? 1 : kManyWaves) * kTile * D / 1024;  // blocks per tile
-  if (L.few) hipLaunchKernelGGL((page_join_kernel<T, D, kTile>), dim3(L.cuts * per), dim3(256), 0, st, k);
-  else hipLaunchKernelGGL((page_join_kernel<T, D, kManyWaves * kTile>), dim3(L.cuts * per), dim3(256), 0, st, k);
+  const dim3 join((unsigned)(L.cuts * (L.tile * D / 1024)));
+  if (L.tile == 16) hipLaunchKernelGGL((page_join_kernel<T, D, 16>), join, dim3(256), 0, st, k);
+  else if (L.few) hipLaunchKernelGGL((page_join_kernel<T, D, 32>), join, dim3(256), 0, st, k);
+  else hipLaunchKernelGGL((page_join_kernel<T, D, kManyWaves * 32>), join, dim3(256), 0, st, k);
   return hipGetLastError();
 }
 
