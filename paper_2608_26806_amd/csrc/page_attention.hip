@@ -755,12 +755,14 @@ __global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void
 }
 
 // Joins the parts of the tiles that were cut: D / 4 threads per row, a block
-// for each 1024 / D rows of a tile.  Where a tile has fewer rows than that, the
+// for each 2048 / D rows of a tile.  Where a tile has fewer rows than that, the
 // groups of threads share out its parts instead.
+constexpr int kJoinThreads = 512;
 template <typename T, int D, int BM>
-__global__ __launch_bounds__(256) void page_join_kernel(KArgs a) {
-  constexpr int TPR = D / 4, GROUPS = 256 / TPR;
-  __shared__ f32x4 x_s[256];
+__global__ __launch_bounds__(kJoinThreads) void page_join_kernel(KArgs a) {
+  constexpr int TPR = D / 4, GROUPS = kJoinThreads / TPR < BM ? kJoinThreads / TPR : BM;
+  constexpr int NT = GROUPS * TPR;  // threads in use
+  __shared__ f32x4 x_s[NT];
   __shared__ float m_s[GROUPS], l_s[GROUPS];
   const Cut t = get_cut(a.meta, blockIdx.x / (BM / GROUPS));
   const int r0 = (blockIdx.x % (BM / GROUPS)) * GROUPS;
@@ -774,26 +776,28 @@ __global__ __launch_bounds__(256) void page_join_kernel(KArgs a) {
   auto part = [&](int s) __attribute__((always_inline)) {
     return (long long)(s == 0 ? t.first : t.next + (s - 1) * t.step) * BM + r;
   };
-  // a running reference: the parts are read once, four at a time
+  // a running reference: the parts are read once, eight at a time
+  constexpr int U = 8;
   float top = -INFINITY, tot = 0.f;
   f32x4 x = f32x4{};
-  for (int s = first; s <= t.more; s += 4 * step) {
-    float ls[4];
-    f32x4 y[4];
+  for (int s = first; s <= t.more; s += U * step) {
+    float ls[U], nm = top;
+    f32x4 y[U];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < U; ++j) {
       const long long at = part(min(s + j * step, t.more));
       ls[j] = s + j * step <= t.more ? a.pl[at] : -INFINITY;
       y[j] = *reinterpret_cast<const f32x4 *>(a.po + at * D + ch * 4);
     }
-    const float nm = fmaxf(top, fmaxf(fmaxf(ls[0], ls[1]), fmaxf(ls[2], ls[3])));
+#pragma unroll
+    for (int j = 0; j < U; ++j) nm = fmaxf(nm, ls[j]);
     const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - nm);
     top = nm;
     tot *= f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) x[k] *= f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < U; ++j) {
       if (ls[j] == -INFINITY) continue;  // nothing in this part (or there is none)
       const float e = __builtin_amdgcn_exp2f(ls[j] - top);
       tot += e;
@@ -891,10 +895,14 @@ static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) 
   else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || L.cuts == 0) return e;
-  const dim3 join((unsigned)(L.cuts * (L.tile * D / 1024)));
-  if (L.tile == 16) hipLaunchKernelGGL((page_join_kernel<T, D, 16>), join, dim3(256), 0, st, k);
-  else if (L.few) hipLaunchKernelGGL((page_join_kernel<T, D, 32>), join, dim3(256), 0, st, k);
-  else hipLaunchKernelGGL((page_join_kernel<T, D, kManyWaves * 32>), join, dim3(256), 0, st, k);
+  // (a block per 2048 / D rows, one for a shorter tile)
+  auto join = [&](auto bm_tag) {
+    constexpr int BM = decltype(bm_tag)::value, ROWS = kJoinThreads * 4 / D < BM ? kJoinThreads * 4 / D : BM;
+    hipLaunchKernelGGL((page_join_kernel<T, D, BM>), dim3((unsigned)(L.cuts * (BM / ROWS))), dim3(ROWS * D / 4), 0, st, k);
+  };
+  if (L.tile == 16) join(std::integral_constant<int, 16>{});
+  else if (L.few) join(std::integral_constant<int, 32>{});
+  else join(std::integral_constant<int, kManyWaves * 32>{});
   return hipGetLastError();
 }
 
