@@ -591,7 +591,8 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   if (WR > 1) __syncthreads();  // the waves are done with the tile before
   auto work = [&](lptr kt, int ks) __attribute__((always_inline)) {
     const lptr vt = kt + TB;
-    if (__builtin_expect(ks + KS <= min(kend, wmin), 1) &&
+    // (the first tiles set the rows' references)
+    if (__builtin_expect(ks > kbeg && ks + KS <= min(kend, wmin), 1) &&
         __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
       return;
     // keys below the range's end, and those that rows of this wave see
