@@ -589,35 +589,52 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 
   const int nstage = kend > kbeg ? (kend - kbeg + KS - 1) / KS : 0;
   if (WR > 1) __syncthreads();  // the waves are done with the tile before
-  auto work = [&](lptr kt, int ks) __attribute__((always_inline)) {
-    const lptr vt = kt + TB;
-    // (the first tiles set the rows' references)
-    if (__builtin_expect(ks > kbeg && ks + KS <= min(kend, wmin), 1) &&
-        __builtin_expect(whole(kt, vt, std::integral_constant<int, TPW>{}), 1))
-      return;
-    // keys below the range's end, and those that rows of this wave see
-    const int stop = min(kend, wmax);
-#pragma unroll 1
-    for (int t = 0; t < TPW; ++t)
-      if (ks + t * kTile < stop) part(kt + t * kTile * ROWB, vt + t * kTile * ROWB, ks + t * kTile);
-  };
   if (nstage > 0) {
     int ids = load_ids(kbeg);
     issue(bufA, kbeg, ids);
     ids = load_ids(kbeg + KS);
-    auto step = [&](lptr buf, AVTP_LDS char *nxt, int st) __attribute__((always_inline)) {
-      const int ks = kbeg + st * KS;
+    // Stage st is in LDS and every wave is done with the other buffer, which
+    // the next stage's loads take.
+    auto begin = [&](AVTP_LDS char *nxt, int st) __attribute__((always_inline)) {
       wait_vmem();
-      if (WR > 1) __syncthreads();  // stage st is in LDS; every wave is done with the other buffer
+      if (WR > 1) __syncthreads();
       if (st + 1 < nstage) {
-        issue(nxt, ks + KS, ids);
-        ids = load_ids(ks + 2 * KS);
+        issue(nxt, kbeg + (st + 1) * KS, ids);
+        ids = load_ids(kbeg + (st + 2) * KS);
       }
-      work(buf, ks);
     };
-    for (int st = 0; st < nstage; st += 2) {
-      step(bufA, bufB, st);
-      if (st + 1 < nstage) step(bufB, bufA, st + 1);
+    // (restrict: the stage read and the one in flight are different memory, or
+    // every read would wait for the loads)
+    auto parts = [&](AVTP_LDS const char *__restrict__ cur, int st) __attribute__((always_inline)) {
+      // keys below the range's end, and those that rows of this wave see
+      const int ks = kbeg + st * KS, stop = min(kend, wmax);
+#pragma unroll 1
+      for (int t = 0; t < TPW; ++t)
+        if (ks + t * kTile < stop) part(cur + t * kTile * ROWB, cur + TB + t * kTile * ROWB, ks + t * kTile);
+    };
+    auto wholes = [&](AVTP_LDS const char *__restrict__ cur, AVTP_LDS char *__restrict__ nxt, int st)
+        __attribute__((always_inline)) {
+      begin(nxt, st);
+      return __builtin_expect(kbeg + (st + 1) * KS <= min(kend, wmin), 1) &&
+             whole(cur, cur + TB, std::integral_constant<int, TPW>{});
+    };
+    // Stages whose keys every row sees run in a loop of their own (with both
+    // kinds in one, O was copied at every stage); the first one, and those that
+    // raise a row's reference, go the other way.
+    begin(bufB, 0);
+    for (int st = 0;;) {
+      parts(bufA, st);
+      bool left = false;
+      while (++st < nstage) {
+        AVTP_LDS char *x = bufA;
+        bufA = bufB;
+        bufB = x;
+        if (!wholes(bufA, bufB, st)) {
+          left = true;
+          break;
+        }
+      }
+      if (!left) break;
     }
   }
   l = over_row<M>(l, [](float x, float y) { return x + y; });
