@@ -371,7 +371,8 @@ int avtp_score_noalloc(avtp_stream_t stream, const avtp_layout *layout, int mode
  * loop can be captured into a graph: tables, store, attention, trim.  Updated
  * lengths and counts go to buffers of their own (outputs must not alias
  * inputs; only block_table, free_pages and the pages are updated in place).
- * B is at most AVTP_MAX_REQUESTS, B * max_pages below 2^31.
+ * B is at most AVTP_MAX_REQUESTS, B * max_pages below 2^31, max_pages *
+ * page_size (a sequence's most tokens) at most 2^30.
  * ---------------------------------------------------------------------- */
 typedef struct {
   void *k, *v;
@@ -456,8 +457,13 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * max_pages * page_size, of which the tokens in the table remain; a negative
  * one is 0.  No atomics on results: reruns are bit-identical.
  * ws: device scratch of avtp_page_attention_workspace_size() bytes (which may
- * be 0, and is for an invalid argument), 256-byte aligned; no initialisation.
- * N_q * Hq is below 2^31, Hq at most 256.
+ * be 0, and is for an invalid argument), 256-byte aligned, no initialisation;
+ * it depends on the sizes alone, so that a call captured at the largest
+ * max_kv_len serves all lengths below.  Calls that may run at the same time
+ * need one each.  N_q * Hq is below 2^31, Hq at most 256.
+ * Speed: with at most 32 rows (tokens times Hq / Hkv) per sequence on average,
+ * the call is bound by reading K and V once; with more, by the products.  A batch of
+ * long chunks and single tokens is best issued as two calls.
  * ---------------------------------------------------------------------- */
 size_t avtp_page_attention_workspace_size(const avtp_pages *pages, int Hq, int B, int64_t N_q,
                                           int64_t max_kv_len);

@@ -435,7 +435,7 @@ static bool page_size_ok(int ps) { return ps >= 16 && ps <= 1024 && (ps & (ps - 
 static int check_tables(int B, int page_size, int max_pages, int n_pages) {
   if (B < 1 || max_pages < 1 || n_pages < 1 || page_size < 1) return AVTP_ERR_INVALID_ARG;
   if (B > AVTP_MAX_REQUESTS || !page_size_ok(page_size)) return AVTP_ERR_UNSUPPORTED;
-  if ((int64_t)B * max_pages > INT32_MAX || (int64_t)max_pages * page_size > INT32_MAX ||
+  if ((int64_t)B * max_pages > INT32_MAX || (int64_t)max_pages * page_size > (1 << 30) ||
       (int64_t)n_pages * page_size > INT32_MAX)
     return AVTP_ERR_UNSUPPORTED;
   return AVTP_OK;

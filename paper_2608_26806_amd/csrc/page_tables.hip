@@ -56,7 +56,7 @@ __device__ inline Need need_of(const TArgs &a, int b) {
   const int ps = a.p.page_shift, mask = (1 << ps) - 1;
   Need r;
   r.L = max(0, a.p.seq_len[b]);
-  r.n = max(0, a.cu_new[b + 1] - a.cu_new[b]);
+  r.n = max(0, max(0, a.cu_new[b + 1]) - max(0, a.cu_new[b]));
   const long long want = ((long long)r.L + r.n + mask) >> ps;
   r.have = (int)(((long long)r.L + mask) >> ps);
   r.room = want <= a.p.max_pages && a.cu_new[b + 1] <= a.n_new;
@@ -115,8 +115,8 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(TArgs a) {
           if (!fits && a.p.status) atomicOr(&a.p.status[b], AVTP_FLAG_NO_PAGES);
         }
         if (here) {
-          cu_s[tid * kPer + j] = a.cu_new[b];
-          if (b + 1 == c1) cu_s[c1 - c0] = a.cu_new[c1];
+          cu_s[tid * kPer + j] = max(0, a.cu_new[b]);
+          if (b + 1 == c1) cu_s[c1 - c0] = max(0, a.cu_new[c1]);
           len_s[tid * kPer + j] = r[j].L;
           off_s[tid * kPer + j] = fits ? off : -1;
         }

@@ -296,3 +296,73 @@ def test_refusals():
     c.scale = math.inf
     with pytest.raises(A.AvtpError):
         c.run()
+
+
+def _reference(c):
+    """out and lse of a large case in float64 on the GPU, a sequence and key head at a time."""
+    N, Hq, d = c.q.shape
+    Hkv, ps = c.pages.Hkv, c.ps
+    out = torch.full((N, Hq, d), float("nan"), dtype=torch.float64, device="cuda")
+    lse = torch.full((Hq, N), float("nan"), dtype=torch.float64, device="cuda")
+    weight, reach = torch.zeros_like(out), torch.zeros_like(lse)
+    for b, (n, L) in enumerate(zip(c.new, c.kv)):
+        if n == 0:
+            continue
+        r0, G = int(c.cu[b]), Hq // Hkv
+        ids = torch.tensor(c.table[b][: -(-L // ps)], device="cuda", dtype=torch.long)
+        hidden = torch.arange(L, device="cuda")[None, :] >= L - n + 1 + torch.arange(n, device="cuda")[:, None]
+        for g in range(Hkv):
+            k, v = (t[ids, g].reshape(-1, d)[:L].double() for t in (c.pages.k, c.pages.v))
+            for h in range(g * G, (g + 1) * G):
+                qq = c.q[r0:r0 + n, h].double()
+                z = (qq @ k.T.contiguous() * c.scale).masked_fill_(hidden, -math.inf)
+                lse[h, r0:r0 + n] = torch.logsumexp(z, 1)
+                p = torch.exp(z - lse[h, r0:r0 + n, None])
+                out[r0:r0 + n, h], weight[r0:r0 + n, h] = p @ v, p @ v.abs()
+                reach[h, r0:r0 + n] = (c.scale * (qq.abs() @ k.abs().T.contiguous())).masked_fill_(hidden, 0).amax(1)
+    f = lambda t: t.cpu().numpy()  # noqa: E731
+    return f(out), f(lse), (f(weight), f(reach))
+
+
+@pytest.mark.parametrize("dtype, d", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+def test_long_chunks_among_single_tokens(dtype, d):
+    # sequences of one row tile beside some of 13 and of 80 tiles, and padding without tokens
+    for B, long in ((65, {3: 100}), (100, {0: 640, 99: 37}), (64, {63: 90}), (1, {0: 9})):
+        new = [long.get(b, b % 3 % 2) for b in range(B)]
+        kv = [n + (53 * b) % 200 for b, n in enumerate(new)]
+        c = Case(B + d, dtype, 4, 2, d, 16, new, kv)
+        c.check(c.run(), _reference(c))
+
+
+@pytest.mark.parametrize("dtype, Hq, Hkv, d", [(torch.bfloat16, 8, 2, 128), (torch.bfloat16, 4, 4, 64),
+                                                (torch.float32, 6, 2, 64), (torch.float32, 4, 1, 128)])
+def test_many_chunks(dtype, Hq, Hkv, d):
+    rng = np.random.default_rng(Hq)
+    for B, low, high, cached in ((70, 40, 60, 300), (64, 40, 60, 300), (7, 200, 500, 1500), (2, 1000, 1300, 0)):
+        new = rng.integers(low, high, B)
+        kv = new + rng.integers(0, cached + 1, B)
+        if B > 60:
+            new[5] = kv[5] = 0
+        c = Case(B, dtype, Hq, Hkv, d, 32, new, kv)
+        c.check(c.run(), _reference(c))
+
+
+def test_long_caches():
+    for new, kv in (([1, 1, 2], [40000, 70001, 513]), ([300], [20000]), ([1] * 9, [3001 + 777 * i for i in range(9)])):
+        c = Case(len(kv), torch.bfloat16, 14, 2, 64, 64, new, kv)
+        ref = _reference(c)
+        c.check(c.run(), ref)
+        c.check(c.run(max_kv=100), ref)
+
+
+def test_first_row_is_not_row_zero():
+    # a batch that starts behind other rows of q and out, few rows and many (more than 64 sequences among them)
+    for B, n in ((3, 1), (3, 70), (66, 40)):
+        c = Case(B, torch.bfloat16, 4, 2, 64, 16, [n] * B, [n + 30] * B, extra_rows=200)
+        out, lse = (t.clone() for t in c.run())
+        q = c.q.roll(150, 0)
+        c.cu = c.cu + 150
+        moved, mlse = c.run(q=q)
+        m = n * B
+        assert torch.equal(moved[150:150 + m], out[:m]) and torch.equal(mlse[:, 150:150 + m], lse[:, :m])
+        assert (moved[:150] == 7.0).all() and (moved[150 + m:] == 7.0).all()
