@@ -145,6 +145,7 @@ hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void
 struct PageAttnPlan {
   bool few;        // few rows per sequence: one wave has them all
   int tile;        // rows of a tile: 16 or 32 (few), 128
+  bool brief;      // few rows and keys: a block per tile, nothing cut
   int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
   int nsplit;      // many: key ranges per tile
   int least;       // few: units (32 keys of a tile) per worker, many: keys per range, at least

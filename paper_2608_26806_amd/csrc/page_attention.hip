@@ -320,9 +320,10 @@ struct Shape {
   static constexpr int kPerSimd = (kPerCu * WR + 3) / 4;
 };
 
-template <typename T, int D, int M, int WR, int TPW>
+// HERE: the part stays in LDS, rows of D floats in bufA and their log2 sums in sums.
+template <typename T, int D, int M, int WR, int TPW, bool HERE = false>
 __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, const Job &job, AVTP_LDS char *bufA,
-                                                             AVTP_LDS char *bufB) {
+                                                             AVTP_LDS char *bufB, AVTP_LDS float *sums = nullptr) {
   using G_ = Geo<T, D>;
   using S_ = Shape<T, D, M, WR, TPW>;
   using M_ = Mma<M>;
@@ -340,9 +341,10 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   const int grp = lane / M, col = lane % M;
   const float cl2e = a.cl2e;
   const int pmask = (1 << a.page_shift) - 1;
+  AVTP_LDS char *const job_buf = bufA;
   const int g = job.g, b = job.b, L = job.s.L, row0 = job.row0, kbeg = job.kbeg, kend = job.kend;
   const int R = job.s.n * a.G;
-  if (L < job.s.kv && a.status && tid == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
+  if (L < job.s.kv && a.status && (WR > 1 ? tid : lane) == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
   // row r of the sequence: token r / G, which sees kv - n + token + 1 keys
   const int wrow = row0 + wave * M;
   const int row = min(wrow + col, R - 1), tok = row / a.G, head = g * a.G + (row - tok * a.G);
@@ -574,12 +576,14 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - nm);
     m = nm;
     l *= f;
+    if (kb > kbeg) {  // (the first tile finds O empty)
 #pragma unroll
-    for (int dt = 0; dt < ND; ++dt)
+      for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-      for (int e = 0; e < AE; ++e) O[dt][e] *= f;
+        for (int e = 0; e < AE; ++e) O[dt][e] *= f;
+    }
     l += probs(S, p, m == -INFINITY ? 0.f : m);  // (no key seen so far: every term is 0)
-    if (__builtin_expect(tile_not_finite(vt), 0)) {
+    if (kb + kTile > min(kend, wmin) && __builtin_expect(tile_not_finite(vt), 0)) {
       add_not_finite(vt, kb);
       weigh(vt, p, true);
     } else {
@@ -637,6 +641,7 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
       if (!left) break;
     }
   }
+  AVTP_LDS char *const part_to = job_buf;
   l = over_row<M>(l, [](float x, float y) { return x + y; });
 
   // the finished rows, or the tile's part
@@ -651,11 +656,13 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     for (int j = 0; j < AE / 4; ++j) {
       const int dd = M * dt + eoff(4 * j) + 4 * grp;
       const f32x4 x = {O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv};
-      if (job.cut) *reinterpret_cast<f32x4 *>(a.po + pr * D + dd) = x;
+      if constexpr (HERE) *reinterpret_cast<AVTP_LDS f32x4 *>(part_to + (col * D + dd) * 4) = x;
+      else if (job.cut) *reinterpret_cast<f32x4 *>(a.po + pr * D + dd) = x;
       else put4<T>(o, dd, x);
     }
   if (grp == 0) {
-    if (job.cut) a.pl[pr] = ls;
+    if constexpr (HERE) sums[col] = ls;
+    else if (job.cut) a.pl[pr] = ls;
     else if (a.lse) a.lse[(long long)head * a.N_q + job.s.q0 + tok] = ls * kLn2;
   }
 }
@@ -704,6 +711,91 @@ __global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_att
   if (threadIdx.x == 0) put_cut(a.meta, worker, c);
 }
 
+// The tile of a rank, -1 if there is none, and its sequence.  The whole wave
+// calls it.
+template <int BM>
+__device__ inline int tile_of_rank(const KArgs &a, int rank, int &b, Seq &s) {
+  const int lane = threadIdx.x & 63;
+  if (a.B <= 64) {
+    // longest sequences first, the tiles that see most first: what is left at
+    // the end is small
+    const Seq mine = seq_of(a, min(lane, a.B - 1));
+    const int nt = lane < a.B ? tiles_of<BM>(a, mine) : 0;
+    int before = 0;
+    for (int j = 0; j < a.B; ++j) {
+      const int kv = __builtin_amdgcn_readlane(mine.L, j), n = __builtin_amdgcn_readlane(nt, j);
+      if (kv > mine.L || (kv == mine.L && j < lane)) before += n;
+    }
+    const u64 m = __ballot(before <= rank && rank < before + nt);
+    if (m == 0) return -1;
+    b = __builtin_ctzll(m);
+    s = uniform(mine, b);
+    return __builtin_amdgcn_readlane(before + nt, b) - 1 - rank;
+  }
+  // Sequence b's tiles have the ranks from floor(q0 G / BM) + b on: the next
+  // sequence's start at least ceil(n G / BM) further, so that no sum over the
+  // sequences is needed.
+  auto start = [&](int x) __attribute__((always_inline)) { return min(max(0, a.cu_q[x]), a.N_q) * a.G / BM + x; };
+  int lo = 0;
+  for (int step = 1 << 12; step > 0; step >>= 6) {  // (B is 2^16 at most)
+    const int x = lo + lane * step;
+    const u64 m = __ballot(x < a.B && start(min(x, a.B - 1)) <= rank);
+    lo += max(0, __builtin_popcountll(m) - 1) * step;
+  }
+  b = lo;
+  s = uniform(seq_of(a, b), 0);
+  const int tile = rank - __builtin_amdgcn_readfirstlane(start(b));
+  return tile < tiles_of<BM>(a, s) ? tile : -1;
+}
+
+// Few rows and few keys: a block takes a whole tile, its W waves a share of the
+// keys each, and joins their parts in LDS: no second launch.
+constexpr int kShortWaves = 4;  // whose buffers a CU's LDS holds
+template <typename T, int D, int M>
+__global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(KArgs a) {
+  using S_ = Shape<T, D, M, 1, 1>;
+  constexpr int KS = S_::KS, BUF = 2 * S_::TB, W = kShortWaves;
+  static_assert(M * D * 4 <= BUF, "a part fits a stage buffer");
+  __shared__ __attribute__((aligned(16))) char smA[W * BUF];
+  __shared__ __attribute__((aligned(16))) char smB[W * BUF];
+  __shared__ float sums[W * M];
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = blockIdx.x % a.Hkv;
+  int b = 0;
+  Seq s{};
+  const int tile = tile_of_rank<M>(a, blockIdx.x / a.Hkv, b, s);
+  if (tile < 0) return;
+  const int keys = tile_keys<M>(a, s, tile), units = units_of<M, KS>(a, s, tile), each = (units + W - 1) / W;
+  const Job job{g, b, tile * M, wave * each * KS, min(keys, (wave + 1) * each * KS), 0, true, s};
+  attend<T, D, M, 1, 1, true>(a, job, (AVTP_LDS char *)smA + wave * BUF, (AVTP_LDS char *)smB + wave * BUF,
+                              (AVTP_LDS float *)sums + wave * M);
+  __syncthreads();
+  constexpr int TPR = D / 4;  // threads per row
+  const int rows = min(s.n * a.G - job.row0, M);
+  for (int i = threadIdx.x; i < rows * TPR; i += 64 * W) {
+    const int r = i / TPR, ch = i % TPR;
+    float top = -INFINITY, tot = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = fmaxf(top, sums[w * M + r]);
+    f32x4 x = f32x4{};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const float ls = sums[w * M + r], f = ls == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ls - top);
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(smA + w * BUF + (r * D + ch * 4) * 4);
+      tot += f;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[k] += y[k] * f;
+    }
+    const float inv = tot == 0.f ? 0.f : 1.f / tot;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] *= inv;
+    const int tok = (job.row0 + r) / a.G, head = g * a.G + (job.row0 + r - tok * a.G);
+    put4<T>(a.out + (s.q0 + tok) * a.out_tok + (long long)head * D * (int)sizeof(T), ch * 4, x);
+    if (ch == 0 && a.lse)
+      a.lse[(long long)head * a.N_q + s.q0 + tok] = tot == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(tot)) * kLn2;
+  }
+}
+
 // Many rows per sequence (chunks of tokens): a block takes one tile of 128 rows
 // of one key head, or one of nsplit ranges of its keys where there are few
 // tiles.  The tiles of one sequence go together, key heads fastest, so that
@@ -716,46 +808,12 @@ __global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void
   constexpr int BM = S_::BM, KS = S_::KS;
   __shared__ __attribute__((aligned(16))) char smA[2 * S_::TB];
   __shared__ __attribute__((aligned(16))) char smB[2 * S_::TB];
-  const int lane = threadIdx.x & 63;
   const int g = blockIdx.x % a.Hkv, rest = blockIdx.x / a.Hkv;
   const int split = rest % a.nsplit, rank = rest / a.nsplit;
   const int place = rank * a.Hkv + g;  // of the tile among all
-  int b = 0, tile = -1;
+  int b = 0;
   Seq s{};
-  if (a.B <= 64) {
-    // longest sequences first, the tiles that see most first: what is left at
-    // the end is small
-    const Seq mine = seq_of(a, min(lane, a.B - 1));
-    const int nt = lane < a.B ? tiles_of<BM>(a, mine) : 0;
-    int before = 0;
-    for (int j = 0; j < a.B; ++j) {
-      const int kv = __builtin_amdgcn_readlane(mine.L, j), n = __builtin_amdgcn_readlane(nt, j);
-      if (kv > mine.L || (kv == mine.L && j < lane)) before += n;
-    }
-    const u64 m = __ballot(before <= rank && rank < before + nt);
-    if (m != 0) {
-      b = __builtin_ctzll(m);
-      s = uniform(mine, b);
-      tile = __builtin_amdgcn_readlane(before + nt, b) - 1 - rank;
-    }
-  } else {
-    // Sequence b's tiles have the ranks from floor(q0 G / BM) + b on: the next
-    // sequence's start at least ceil(n G / BM) further, so that no sum over the
-    // sequences is needed.
-    auto start = [&](int x) __attribute__((always_inline)) {
-      return min(max(0, a.cu_q[x]), a.N_q) * a.G / BM + x;
-    };
-    int lo = 0;
-    for (int step = 1 << 12; step > 0; step >>= 6) {  // (B is 2^16 at most)
-      const int x = lo + lane * step;
-      const u64 m = __ballot(x < a.B && start(min(x, a.B - 1)) <= rank);
-      lo += max(0, __builtin_popcountll(m) - 1) * step;
-    }
-    b = lo;
-    s = uniform(seq_of(a, b), 0);
-    tile = rank - __builtin_amdgcn_readfirstlane(start(b));
-    if (tile >= tiles_of<BM>(a, s)) tile = -1;
-  }
+  const int tile = tile_of_rank<BM>(a, rank, b, s);
   Cut c{};
   if (tile >= 0) {
     const int keys = tile_keys<BM>(a, s, tile);
@@ -853,6 +911,13 @@ __global__ __launch_bounds__(kJoinThreads) void page_join_kernel(KArgs a) {
 }
 
 constexpr int kManyWaves = 4;
+// Few rows and few keys in bf16: a block per tile that joins its waves' parts
+// itself, while the tiles fit on the chip at once (320 for 32 requests of 8 key
+// heads) and four waves are enough for a tile's keys.  One request, 28/4 heads of
+// 128: 793 keys 10.3 -> 8.9 us, 1,500 keys 12.0 -> 12.6; 32 requests of 300 keys,
+// 32/8 heads, 16.2 -> 12.7, 64 of them 19.9 -> 31.3.  fp32 keeps the line: 8 requests
+// of 300 keys 16.6 -> 19.3.
+constexpr int kShortTiles = 384, kShortKeys = 1024;
 // 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
 constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
@@ -860,17 +925,20 @@ constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
 PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len) {
   PageAttnPlan L{};
-  const int row_bytes = P.d * (P.dtype == AVTP_FP32 ? 4 : 2);
   // (longer sequences run all the same)
   max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
   const int64_t rows = N_q * (Hq / P.Hkv);
   // one wave of 16 or 32 rows for a sequence, or blocks of 128
   L.few = rows <= (int64_t)B * 32;
   const int bm = L.tile = rows <= (int64_t)B * 16 ? 16 : L.few ? 32 : kManyWaves * 32;
-  // (at most; many of more than 64 sequences: the ranks the kernel gives them)
-  const int64_t tiles = (rows / bm + (L.few && N_q < B ? N_q : B)) * P.Hkv;
+  // (at most: the ranks that the kernels give them)
+  const int64_t tiles = (rows / bm + B) * P.Hkv;
+  L.brief = L.few && P.dtype == AVTP_BF16 && tiles <= kShortTiles && max_kv_len <= kShortKeys;
   int64_t slots;
-  if (L.few) {
+  if (L.brief) {
+    L.blocks = tiles;
+    slots = 0;
+  } else if (L.few) {
     // as many workers as the CUs' LDS holds; fewer where there is less work than
     // `least` units (a tile's 32 keys) for each
     auto per_cu = [&](auto m_tag) {
@@ -885,10 +953,13 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     L.cuts = (int)L.blocks;
     slots = 2 * L.blocks;
   } else {
-    // two blocks per CU (one of fp32 rows of 512 bytes), of 256 keys or more (64
-    // in fp32, whose products take 16 times as long)
-    const int64_t want = row_bytes > 256 ? 256 : 512;
-    L.least = P.dtype == AVTP_FP32 ? 64 : 256;
+    // Two blocks per CU, of 256 keys or more.  In fp32, whose products take 16
+    // times as long, four (two of 512-byte rows) of 64 or more: one chunk of 1,000
+    // tokens, 16/8 heads of 128, 85 us with half as many, 70 with these, 88 with
+    // twice as many.  (bf16 with twice as many: four chunks of 300 tokens 20 -> 31.)
+    const bool f32 = P.dtype == AVTP_FP32;
+    const int64_t want = f32 && P.d == 64 ? 1024 : 512;
+    L.least = f32 ? 64 : 256;
     const int64_t most = (max_kv_len + L.least - 1) / L.least;
     const int64_t ns = tiles < 1 ? 1 : want / tiles;
     L.nsplit = (int)(ns < 1 ? 1 : ns < most ? ns : most);
@@ -908,6 +979,13 @@ template <typename T, int D>
 static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) {
   constexpr int TPW = many_tiles(D * (int)sizeof(T));
   const dim3 grid((unsigned)L.blocks);
+  if constexpr (sizeof(T) == 2) {
+    if (L.brief) {
+      if (L.tile == 16) hipLaunchKernelGGL((page_attn_short_kernel<T, D, 16>), grid, dim3(64 * kShortWaves), 0, st, k);
+      else hipLaunchKernelGGL((page_attn_short_kernel<T, D, 32>), grid, dim3(64 * kShortWaves), 0, st, k);
+      return hipGetLastError();
+    }
+  }
   if (L.tile == 16) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 16>), grid, dim3(64), 0, st, k);
   else if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 32>), grid, dim3(64), 0, st, k);
   else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);

@@ -103,9 +103,11 @@ def test_workspace_size():
     size = lambda Hq, B, N, kv, **p: A.lib().avtp_page_attention_workspace_size(  # noqa: E731
         ctypes.byref(_pages(**p)), Hq, B, N, kv)
     assert size(4, 2, 0, 1 << 20) == 0
-    one = size(4, 1, 1, 64)
-    assert one >= 2 * 32 * (128 + 1) * 4                             # the parts of one cut tile
+    assert size(4, 2, 6, 64) == 0                                    # few rows and keys: nothing is cut
+    one = size(4, 1, 1, 2000)
+    assert one >= 2 * 16 * (128 + 1) * 4                             # the parts of one cut tile
     assert one <= size(4, 1, 1, 1 << 20) == size(4, 1, 2, 1 << 20)   # as many workers as the chip holds
+    assert size(4, 1, 1, 64, dtype=A.FP32) > 0
     assert size(4, 1, 9000, 1 << 20) == 0                            # chunks that fill the chip uncut
     assert size(4, 1, 100, 1 << 20) >= 2 * 128 * (128 + 1) * 4       # and one that does not
     assert size(3, 1, 1, 64) == 0 and size(4, 0, 1, 64) == 0 and size(4, 1, 1, -1) == 0
