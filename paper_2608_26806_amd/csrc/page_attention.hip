@@ -543,22 +543,85 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
       }
     }
   };
-  // N tiles of 32 keys that every row of the wave sees.  false (nothing done):
-  // a row's sum left its range, or has no reference yet; `part` takes them.
-  auto whole = [&](lptr kt, lptr vt, auto n_tag) __attribute__((always_inline)) {
-    constexpr int N = decltype(n_tag)::value;
-    Logits S[N];
-    Probs p[N];
-    float tot = 0.f;
+  // A stage whose keys every row of the wave sees.  Returns how many of its tiles
+  // are done: at the first one that takes a row's sum out of its range (or finds
+  // no reference yet) it stops, and `part` takes the rest.
+  auto whole = [&](lptr kt, lptr vt) __attribute__((always_inline)) {
+    if constexpr (TPW == 2 && M == 32 && !F32) {
+      // Two tiles, the matrix core and the VALU at work together: tile 1's logits
+      // beside tile 0's exponentials, tile 0's products with V beside tile 1's.  One
+      // MFMA a step, with the LDS read of the step two further on and some
+      // exponentials; left to itself the compiler puts all products of a kind
+      // first.  32/8 heads of 128, four prompts of 7,000-9,000 tokens 2050 -> 2011 us
+      // (1075 TFLOP/s); 28/4 heads, two of 2,048 83.2 -> 79.9; 14/2 heads of 64, 16 of
+      // 1,000 66.0 -> 64.4.
+      constexpr int AHEAD = 2, STEPS = 2 * ND;
+      Logits S[2];
+      Probs p[2];
+      float sum[2][2] = {{0.f, 0.f}, {0.f, 0.f}};
+      auto terms = [&](int i, int e0, int e1) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) S[i] = logits(kt + i * kTile * ROWB);
+        for (int e = e0; e < e1; ++e) {
+          const float x = __builtin_amdgcn_exp2f(S[i].get(e) * cl2e - m);
+          sum[i][e & 1] += x;
+          p[i].x[e >> 3][e & 7] = (__bf16)x;
+        }
+      };
+      auto step_end = []() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
+      bf16x8 kf[AHEAD], vf[AHEAD];
+      auto kread = [&](int i) __attribute__((always_inline)) {
+        return *reinterpret_cast<AVTP_LDS const bf16x8 *>(kaddr(kt + i / NS * kTile * ROWB, 0, i % NS));
+      };
+      auto vread = [&](int j) __attribute__((always_inline)) {
+        return vfrag(vt + j / STEPS * kTile * ROWB, j / ND % 2, j % ND);
+      };
+      auto product = [&](int j) __attribute__((always_inline)) {
+        O[j % ND] = M_::run(vf[j % AHEAD], p[j / STEPS].x[j / ND % 2], O[j % ND]);
+        if (j + AHEAD < 2 * STEPS) vf[j % AHEAD] = vread(j + AHEAD);
+      };
 #pragma unroll
-    for (int i = 0; i < N; ++i) tot += probs(S[i], p[i], m);
-    if (__builtin_expect(__ballot(!(tot <= kLazyLimit)) != 0ull, 0)) return false;
-    l += tot;
+      for (int i = 0; i < AHEAD; ++i) kf[i] = kread(i);
+      step_end();
 #pragma unroll
-    for (int i = 0; i < N; ++i) weigh(vt + i * kTile * ROWB, p[i], false);
-    return true;
+      for (int i = 0; i < 2 * NS; ++i) {
+        f32x16 &x = S[i / NS].x[0];
+        x = M_::run(kf[i % AHEAD], __builtin_bit_cast(bf16x8, qf[i % NS]), i % NS == 0 ? f32x16{} : x);
+        if (i + AHEAD < 2 * NS) kf[i % AHEAD] = kread(i + AHEAD);
+        else vf[i + AHEAD - 2 * NS] = vread(i + AHEAD - 2 * NS);
+        if (i > NS) terms(0, (i - NS - 1) * 16 / (NS - 1), (i - NS) * 16 / (NS - 1));
+        step_end();
+      }
+      const float t0 = sum[0][0] + sum[0][1];
+      if (__builtin_expect(__ballot(!(t0 <= kLazyLimit)) != 0ull, 0)) return 0;
+      l += t0;
+#pragma unroll
+      for (int j = 0; j < STEPS; ++j) {
+        product(j);
+        terms(1, j * 16 / STEPS, (j + 1) * 16 / STEPS);
+        step_end();
+      }
+      const float t1 = sum[1][0] + sum[1][1];
+      if (__builtin_expect(__ballot(!(t1 <= kLazyLimit)) != 0ull, 0)) return 1;
+      l += t1;
+#pragma unroll
+      for (int j = STEPS; j < 2 * STEPS; ++j) {
+        product(j);
+        step_end();
+      }
+    } else {
+      Logits S[TPW];
+      Probs p[TPW];
+      float tot = 0.f;
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) S[i] = logits(kt + i * kTile * ROWB);
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) tot += probs(S[i], p[i], m);
+      if (__builtin_expect(__ballot(!(tot <= kLazyLimit)) != 0ull, 0)) return 0;
+      l += tot;
+#pragma unroll
+      for (int i = 0; i < TPW; ++i) weigh(vt + i * kTile * ROWB, p[i], false);
+    }
+    return TPW;
   };
   // A tile of keys from kb on, of which some rows may see a part or nothing, and
   // whose largest logit becomes the row's reference if it is larger.
@@ -609,39 +672,35 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     };
     // (restrict: the stage read and the one in flight are different memory, or
     // every read would wait for the loads)
-    auto parts = [&](AVTP_LDS const char *__restrict__ cur, int st) __attribute__((always_inline)) {
+    auto parts = [&](AVTP_LDS const char *__restrict__ cur, int st, int from) __attribute__((always_inline)) {
       // keys below the range's end, and those that rows of this wave see
       const int ks = kbeg + st * KS, stop = min(kend, wmax);
 #pragma unroll 1
-      for (int t = 0; t < TPW; ++t)
+      for (int t = from; t < TPW; ++t)
         if (ks + t * kTile < stop) part(cur + t * kTile * ROWB, cur + TB + t * kTile * ROWB, ks + t * kTile);
     };
     auto wholes = [&](AVTP_LDS const char *__restrict__ cur, AVTP_LDS char *__restrict__ nxt, int st)
         __attribute__((always_inline)) {
       begin(nxt, st);
-      return __builtin_expect(kbeg + (st + 1) * KS <= min(kend, wmin), 1) &&
-             whole(cur, cur + TB, std::integral_constant<int, TPW>{});
+      return __builtin_expect(kbeg + (st + 1) * KS <= min(kend, wmin), 1) ? whole(cur, cur + TB) : 0;
     };
     // Stages whose keys every row sees run in a loop of their own (with both
     // kinds in one, O was copied at every stage); the first one, and those that
     // raise a row's reference, go the other way.
     begin(bufB, 0);
+    int done = 0;  // tiles of stage st
     for (int st = 0;;) {
-      parts(bufA, st);
-      bool left = false;
-      while (++st < nstage) {
+      parts(bufA, st, done);
+      done = TPW;
+      while (done == TPW && ++st < nstage) {
         AVTP_LDS char *x = bufA;
         bufA = bufB;
         bufB = x;
-        if (!wholes(bufA, bufB, st)) {
-          left = true;
-          break;
-        }
+        done = wholes(bufA, bufB, st);
       }
-      if (!left) break;
+      if (done == TPW) break;
     }
   }
-  AVTP_LDS char *const part_to = job_buf;
   l = over_row<M>(l, [](float x, float y) { return x + y; });
 
   // the finished rows, or the tile's part
@@ -656,7 +715,7 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     for (int j = 0; j < AE / 4; ++j) {
       const int dd = M * dt + eoff(4 * j) + 4 * grp;
       const f32x4 x = {O[dt][4 * j] * inv, O[dt][4 * j + 1] * inv, O[dt][4 * j + 2] * inv, O[dt][4 * j + 3] * inv};
-      if constexpr (HERE) *reinterpret_cast<AVTP_LDS f32x4 *>(part_to + (col * D + dd) * 4) = x;
+      if constexpr (HERE) *reinterpret_cast<AVTP_LDS f32x4 *>(job_buf + (col * D + dd) * 4) = x;
       else if (job.cut) *reinterpret_cast<f32x4 *>(a.po + pr * D + dd) = x;
       else put4<T>(o, dd, x);
     }
@@ -686,8 +745,7 @@ __global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_att
     per += wave::sum(seq_units<BM, KS>(a, c0, x));
   }
   const u64 all = per * (unsigned)a.Hkv;
-  u64 share = (all + a.workers - 1) / a.workers;
-  if (share < (unsigned)a.least) share = a.least;
+  const u64 share = (all + a.workers - 1) / a.workers;
   u64 w = share * worker;
   const u64 wend = w + share < all ? w + share : all;
   Cut c{};
@@ -939,16 +997,15 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     L.blocks = tiles;
     slots = 0;
   } else if (L.few) {
-    // as many workers as the CUs' LDS holds; fewer where there is less work than
-    // `least` units (a tile's 32 keys) for each
+    // as many workers as the CUs' LDS holds, but no more than there are units (of
+    // 32 keys)
     auto per_cu = [&](auto m_tag) {
       constexpr int M = decltype(m_tag)::value;
       if (P.dtype == AVTP_FP32) return P.d == 64 ? Shape<float, 64, M, 1, 1>::kPerCu : Shape<float, 128, M, 1, 1>::kPerCu;
       return P.d == 64 ? Shape<__bf16, 64, M, 1, 1>::kPerCu : Shape<__bf16, 128, M, 1, 1>::kPerCu;
     };
     const int64_t most = 256 * (bm == 16 ? per_cu(std::integral_constant<int, 16>{}) : per_cu(std::integral_constant<int, 32>{}));
-    L.least = 1;
-    const int64_t need = (tiles * ((max_kv_len + kTile - 1) / kTile) + L.least - 1) / L.least;
+    const int64_t need = tiles * ((max_kv_len + kTile - 1) / kTile);
     L.blocks = need < most ? need : most;
     L.cuts = (int)L.blocks;
     slots = 2 * L.blocks;
