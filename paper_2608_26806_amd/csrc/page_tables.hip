@@ -196,16 +196,19 @@ __global__ __launch_bounds__(kThreads) void page_trim_kernel(RArgs a) {
   // lane j: the block's sequence j (every wave holds them all)
   Back r{0, 0, 0};
   if (b0 + lane < b1) r = back_of(a, b0 + lane);
-  const int end = count + before + (int)wave::prefix_sum((uint32_t)r.n);
+  // (B * max_pages pages handed back onto n_pages: below 2^32)
+  const uint32_t end = (uint32_t)count + (uint32_t)before + wave::prefix_sum((uint32_t)r.n);
+  const uint32_t cap = (uint32_t)a.p.n_pages;
   for (int j = wave; j < b1 - b0; j += kWaves) {
-    const int n = __builtin_amdgcn_readlane(r.n, j), at = __builtin_amdgcn_readlane(end, j) - n;
-    const int m = min(n, max(0, a.p.n_pages - at));
+    const int n = __builtin_amdgcn_readlane(r.n, j);
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)end, j) - (uint32_t)n;
+    const int m = at < cap ? (int)min((uint32_t)n, cap - at) : 0;
     const int32_t *row = a.table + (size_t)(b0 + j) * a.p.max_pages + __builtin_amdgcn_readlane(r.first, j);
     for (int i = lane; i < m; i += 64) a.free_pages[at + i] = row[i];
     if (m < n && lane == 0 && a.p.status) atomicOr(&a.p.status[b0 + j], AVTP_FLAG_OUT_CAPACITY);
   }
   if (wave == 0 && b0 + lane < b1) a.p.seq_len_out[b0 + lane] = r.keep;
-  if (b1 == B && tid == 63) a.p.free_count_out[0] = min(end, a.p.n_pages);
+  if (b1 == B && tid == 63) a.p.free_count_out[0] = (int)min(end, cap);
 }
 
 }  // namespace

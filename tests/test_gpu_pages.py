@@ -118,6 +118,19 @@ def test_trim_into_a_full_stack_flags():
     assert status.tolist() == rs.tolist() == [0, P.FLAG_OUT_CAPACITY, P.FLAG_OUT_CAPACITY]
 
 
+def test_trim_of_more_pages_than_31_bits():
+    # the pages handed back and the stack together pass 2^31: 31 sequences of 2^30 tokens
+    B, per, n_pages = 31, 1 << 26, (1 << 27) - 1
+    say("[page trim] 31 x 2^26 pages")
+    table = torch.zeros(B, per, dtype=torch.int32, device="cuda")
+    table[0, :100] = torch.arange(100, device="cuda", dtype=torch.int32) + 7
+    f = torch.full((n_pages,), -3, dtype=torch.int32, device="cuda")
+    status = torch.zeros(B, dtype=torch.int32, device="cuda")
+    out, left = A.page_trim(16, ints([0] * B), ints([1 << 30] * B), table, f, ints([n_pages - 100]), status=status)
+    assert int(left) == n_pages and not out.any() and (status == A.FLAG_OUT_CAPACITY).all()
+    assert torch.equal(f[-100:], table[0, :100]) and (f[:-100] == -3).all()
+
+
 def _bits(t):
     return t.view(torch.int32 if t.element_size() == 4 else torch.int16).cpu().numpy()
 
