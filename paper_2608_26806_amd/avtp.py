@@ -7,6 +7,7 @@ library is missing, loading it raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 import re
@@ -635,6 +636,16 @@ def _page_arg(t: Optional[torch.Tensor], name: str, numel: int = 0, dtype=torch.
     return _arg(t, name, numel, dtype)
 
 
+def _on(stream, device):
+    """What a call on ``stream`` allocates belongs to that stream: a workspace of
+    the current one would be handed on while the call still uses it."""
+    if stream is None or device.type != "cuda":  # (host tensors: refused below)
+        return contextlib.nullcontext()
+    if isinstance(stream, ctypes.c_void_p):
+        stream = torch.cuda.ExternalStream(stream.value or 0)
+    return torch.cuda.stream(stream)
+
+
 def _page_rows(t: torch.Tensor, name: str, heads: int, pages: "Pages"):
     """Pointer and token stride of rows [N, heads, d] (a slice of a fused
     projection is fine: only the token stride is free)."""
@@ -706,7 +717,8 @@ def page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Tensor, fre
     """Room for the new tokens of every request (block_table is updated in
     place).  Returns (slot_map [n_new], seq_len_out, free_count_out)."""
     new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
-    slot_map, seq_len_out, free_count_out = new(n_new), new(seq_len.numel()), new(1)
+    with _on(stream, seq_len.device):
+        slot_map, seq_len_out, free_count_out = new(n_new), new(seq_len.numel()), new(1)
     prepare_page_tables(page_size, cu_new, seq_len, free_pages, free_count, block_table, slot_map,
                         seq_len_out, free_count_out, status, stream)()
     return slot_map, seq_len_out, free_count_out
@@ -736,7 +748,8 @@ def page_trim(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor, blo
     longer needs (free_pages is updated in place).  Returns (seq_len_out,
     free_count_out)."""
     new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
-    seq_len_out, free_count_out = new(seq_len.numel()), new(1)
+    with _on(stream, seq_len.device):
+        seq_len_out, free_count_out = new(seq_len.numel()), new(1)
     prepare_page_trim(page_size, keep_len, seq_len, block_table, free_pages, free_count, seq_len_out,
                       free_count_out, status, stream)()
     return seq_len_out, free_count_out
@@ -804,13 +817,14 @@ def page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: to
     N, Hq, _ = q.shape
     if max_kv_len is None:
         max_kv_len = block_table.shape[-1] * pages.page_size
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if lse is None:
-        lse = torch.empty((Hq, N), dtype=torch.float32, device=q.device)
-    if ws is None:
-        ws = alloc_workspace(page_attention_workspace_bytes(pages, Hq, kv_len.numel(), N, max_kv_len),
-                             q.device)
+    with _on(stream, q.device):
+        if out is None:
+            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        if lse is None:
+            lse = torch.empty((Hq, N), dtype=torch.float32, device=q.device)
+        if ws is None:
+            ws = alloc_workspace(page_attention_workspace_bytes(pages, Hq, kv_len.numel(), N, max_kv_len),
+                                 q.device)
     prepare_page_attention(pages, q, cu_q, kv_len, block_table, softmax_scale, max_kv_len, out, ws,
                            lse, status, stream)()
     return out, lse

@@ -8,6 +8,7 @@ moves by the logit's error and the sum's relative one, plus its own rounding.
 An output is sum p v / sum p: p's relative errors count twice (numerator and
 sum) on sum p |v| (`weight`); bf16 rounds p once more (2^-8 of it) and the
 result once (2^-8 of it); the chain over the keys rounds n / 16 + 20 times."""
+import ctypes
 import math
 
 import numpy as np
@@ -245,6 +246,31 @@ def test_reruns_streams_and_two_calls_at_once():
             res.append((other, e.run()))
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for x, y in res for a, b in zip(x, y))
+
+
+def test_a_workspace_belongs_to_the_stream_of_its_call(monkeypatch):
+    # a stream named in the call: its workspace must not go to the current
+    # stream's next allocation while the call may still be running
+    c = Case(43, torch.bfloat16, 28, 4, 128, 16, [1, 1], [3000, 1500])
+    args = (c.pages, c.q, ints(c.cu), ints(c.kv), ints(c.table), c.scale, 3000)
+    first = A.page_attention(*args)
+    torch.cuda.synchronize()
+    s, alloc, spans = torch.cuda.Stream(), A.alloc_workspace, []
+
+    def noted(*args):
+        ws = alloc(*args)
+        spans.append((ws.data_ptr(), ws.numel()))
+        return ws
+
+    monkeypatch.setattr(A, "alloc_workspace", noted)
+    for stream in (s, ctypes.c_void_p(s.cuda_stream)):
+        say(f"[page attention] on {stream}")
+        got = A.page_attention(*args, stream=stream)
+        ptr, n = spans[-1]
+        assert not ptr <= alloc(n).data_ptr() < ptr + n
+        torch.cuda.synchronize()
+        n_tok = int(c.cu[-1])                                     # (other rows are left as they were)
+        assert torch.equal(got[0][:n_tok], first[0][:n_tok]) and torch.equal(got[1][:, :n_tok], first[1][:, :n_tok])
 
 
 def test_two_captured_graphs_with_growing_lengths():
