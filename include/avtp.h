@@ -460,7 +460,8 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * be 0, and is for an invalid argument), 256-byte aligned, no initialisation;
  * it depends on the sizes alone, so that a call captured at the largest
  * max_kv_len serves all lengths below.  Calls that may run at the same time
- * need one each.  N_q * Hq is below 2^31, Hq at most 256.
+ * need one each.  N_q * Hq is below 2^31, Hq at most 256, and with more than 32
+ * rows per sequence N_q * Hq / 128 + B * Hkv below 2^24.
  * Speed: with at most 32 rows (tokens times Hq / Hkv) per sequence on average,
  * the call is bound by reading K and V once; with more, by the products.  A batch of
  * long chunks and single tokens is best issued as two calls.

@@ -516,6 +516,8 @@ static int check_page_attention(const avtp_pages *pages, int Hq, int B, int64_t 
   if ((rc = check_attn_args(pages->dtype, Hq, pages->Hkv, pages->d)) != AVTP_OK) return rc;
   if (B < 1 || N_q < 0 || max_kv_len < 0) return AVTP_ERR_INVALID_ARG;
   if (B > AVTP_MAX_REQUESTS || N_q > INT32_MAX / Hq) return AVTP_ERR_UNSUPPORTED;
+  // blocks of 256 threads, of which a launch has fewer than 2^32
+  if (page_attn_plan(*pages, Hq, B, N_q, max_kv_len).blocks >= 1 << 24) return AVTP_ERR_UNSUPPORTED;
   return AVTP_OK;
 }
 

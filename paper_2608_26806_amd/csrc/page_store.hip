@@ -33,7 +33,8 @@ struct SArgs {
 
 __global__ __launch_bounds__(kThreads) void page_store_kernel(SArgs a) {
   const int lane = threadIdx.x & ((1 << a.lpr_shift) - 1);
-  const long long r = (long long)blockIdx.x * (kThreads >> a.lpr_shift) + (threadIdx.x >> a.lpr_shift);
+  const long long block = (long long)blockIdx.y * gridDim.x + blockIdx.x;
+  const long long r = block * (kThreads >> a.lpr_shift) + (threadIdx.x >> a.lpr_shift);
   if (r >= a.n) return;
   const long long s = a.slot[r], j = a.keep ? a.keep[r] : r;
   if (s < 0 || s >= a.slots || j < 0 || j >= a.n_src) return;
@@ -73,8 +74,10 @@ hipError_t launch_page_store(hipStream_t st, const avtp_pages &P, const void *k,
   a.page_shift = __builtin_ctz((unsigned)P.page_size);
   a.Hkv = P.Hkv;
   a.slots = (long long)P.n_pages * P.page_size;
-  const long long rows = kThreads >> a.lpr_shift;
-  hipLaunchKernelGGL(page_store_kernel, dim3((unsigned)((n + rows - 1) / rows)), dim3(kThreads), 0, st, a);
+  const long long rows = kThreads >> a.lpr_shift, blocks = (n + rows - 1) / rows;
+  constexpr long long kWide = 1 << 20;  // blocks side by side (2^32 threads are too many for one axis)
+  const dim3 grid((unsigned)(blocks < kWide ? blocks : kWide), (unsigned)((blocks + kWide - 1) / kWide));
+  hipLaunchKernelGGL(page_store_kernel, grid, dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 

@@ -169,6 +169,24 @@ def test_store_behind_4_gib():
         assert torch.equal(pages.v[s // 128, :, s % 128], rows[r] * 2)
 
 
+def test_store_of_more_rows_than_one_axis_has():
+    # a block per row: 2^24 + 100 of them, few with a place
+    n = (1 << 24) + 100
+    pages = A.Pages(*(torch.zeros(2, 16, 16, 128, dtype=torch.bfloat16, device="cuda") for _ in "kv"))
+    rows = torch.randn(3, 16, 128, device="cuda").to(torch.bfloat16)
+    slots = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    keep = torch.zeros(n, dtype=torch.int32, device="cuda")
+    at = [(0, 5, 1), ((1 << 20) + 3, 0, 2), (1 << 24, 31, 0), (n - 1, 16, 2)]   # row, slot, source
+    for r, s, j in at:
+        slots[r], keep[r] = s, j
+    say(f"[page store] {n} rows")
+    A.page_store(pages, rows, -rows, slots, keep)
+    want = torch.zeros_like(pages.k)
+    for _, s, j in at:
+        want[s // 16, :, s % 16] = rows[j]
+    assert torch.equal(pages.k, want) and torch.equal(pages.v, -want)
+
+
 def test_binding_refuses_bad_tensors():
     pages = A.Pages.empty(4, 2, 16, 64)
     rows = torch.zeros(6, 2, 64, dtype=torch.bfloat16, device="cuda")

@@ -92,6 +92,15 @@ def test_attention_refusals(pages, patch, rc):
     assert A.lib().avtp_page_attention(*a.values()) == rc
 
 
+def test_attention_refuses_more_blocks_than_a_launch_has():
+    # 2^16 sequences of 256 key heads: half of the blocks for the rows, half for tiles' ends
+    for N_q in (1 << 22, (1 << 31) // 256 - 1):
+        a = {**ATT, "pages": ctypes.byref(_pages(Hkv=256)), "Hq": 256, "B": 1 << 16, "N_q": N_q, "qs": 1 << 15,
+             "os": 1 << 15}
+        assert A.lib().avtp_page_attention(*a.values()) == U
+        assert A.lib().avtp_page_attention_workspace_size(a["pages"], 256, 1 << 16, N_q, 64) == 0
+
+
 def test_null_pool():
     lib = A.lib()
     assert lib.avtp_page_store(*{**STORE, "pages": None}.values()) == I
