@@ -6,8 +6,9 @@ layers between two pruning layers share their lengths and no others do.  A
 ``PagedCache`` is the cache of such a group of layers: one block table, one
 stack of free pages, and each layer's pages.
 
-    slots = cache.reserve(cu_out, dl.N_out)            # room for the kept tokens
-    cache.store(layer, k, v, slots, keep_idx=keep)     # their K and V, picked on the way
+    cache.reserve(cu_out, dl.N_out)                    # room for the kept tokens
+    cache.store(0, k, v, keep_idx=keep)                # their K and V, picked on the way
+    cache.store(1, k1, v1)                             # the next layer's, of the kept tokens
     out, lse = cache.attend(layer, q, cu_q, scale)     # new tokens over the cache
     cache.trim(keep_len)                               # requests that ended, drafts taken back
 
@@ -40,21 +41,29 @@ class PagedCache:
         self.block_table = ints(requests, max_pages) - 1
         self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
         self.free_count.fill_(n_pages)
+        self.slots: Optional[torch.Tensor] = None  # of the tokens reserved last
 
     def reserve(self, cu_new: torch.Tensor, n_new: int, slot_map: Optional[torch.Tensor] = None,
                 status: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Room for cu_new[b+1] - cu_new[b] more tokens of every sequence;
-        returns their slots (n_new entries, -1 where a request got no place)."""
+        """Room for cu_new[b+1] - cu_new[b] more tokens of every sequence, in
+        every layer; returns their slots (n_new entries, -1 where a request got
+        no place), which ``store`` takes by default."""
         if slot_map is None:
             slot_map = torch.empty(n_new, dtype=torch.int32, device=cu_new.device)
         B = self.seq_len.numel()
         A.prepare_page_tables(self.page_size, cu_new, self.seq_len, self.free_pages, self.free_count,
                               self.block_table, slot_map, self._after[:B], self._after[B:], status)()
         self._state.copy_(self._after)
+        self.slots = slot_map
         return slot_map
 
-    def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor,
+    def store(self, layer: int, k: torch.Tensor, v: torch.Tensor, slot_map: Optional[torch.Tensor] = None,
               keep_idx: Optional[torch.Tensor] = None) -> None:
+        """A layer's K and V of the tokens reserved last (or of ``slot_map``)."""
+        if slot_map is None:
+            slot_map = self.slots
+        if slot_map is None:
+            raise ValueError("no tokens have been reserved")
         A.page_store(self.layers[layer], k, v, slot_map, keep_idx)
 
     def attend(self, layer: int, q: torch.Tensor, cu_q: torch.Tensor, softmax_scale: float,

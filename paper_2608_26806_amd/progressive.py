@@ -55,11 +55,23 @@ class ProgressivePruner:
         """Prune at one layer.  others: (tensor, token_dim) pairs compacted with
         h_cur.  cache (a PagedCache with a row for every sequence of the batch)
         takes the kept rows of the layer's k and v [N_tok, Hkv, d] behind what
-        its sequences hold already, into the pages of its layer ``layer``.
+        its sequences hold already, into the pages of its layer ``layer``; the
+        layers up to the next pruning one store theirs in the same slots
+        (``cache.store(layer + 1, k, v)``, of the kept tokens).
         Returns (h_out, [compacted others], keep_idx, budget, scores, img_sum);
         afterwards self.dl is the next layer's layout (keep totals from
         keep_pct_next) and self.h_prior is h_out."""
         dl = self.dl
+        if cache is not None:
+            # (a call that fails behind the reservation would leave places without K and V)
+            pages = cache.layers[layer]
+            want = (dl.N_tok, pages.Hkv, pages.d)
+            for name, t in (("k", k), ("v", v)):
+                if t is None or tuple(t.shape) != want or t.dtype != pages.dtype:
+                    raise ValueError(f"{name}: {list(want)} of {pages.dtype} is needed, got "
+                                     f"{t if t is None else (list(t.shape), t.dtype)}")
+            if cache.seq_len.numel() != dl.B:
+                raise ValueError(f"the cache has {cache.seq_len.numel()} sequences, the batch {dl.B}")
         scores, isum = A.score_variation(dl, h_cur, self.h_prior, status=status)
         pairs = []
         for src, tdim in [(h_cur, 0), *others]:

@@ -132,6 +132,30 @@ def test_shortage_is_flagged_and_changes_nothing():
     assert int(cache.free_count) == 1 and torch.equal(cache.block_table, state[2])
 
 
+def test_a_pruning_step_refuses_before_it_reserves_and_its_slots_serve_the_next_layer():
+    dl = A.DeviceLayout(build_layout([[40, 20], [30]], 3, 12, 50))
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda").to(torch.bfloat16)  # noqa: E731
+    cur, k, v = rnd(dl.N_tok, 64), rnd(dl.N_tok, 2, 64), rnd(dl.N_tok, 2, 64)
+    pruner = ProgressivePruner(dl, rnd(dl.N_tok, 64))
+    cache = PagedCache(dl.B, n_pages=20, max_pages=10, Hkv=2, d=64, page_size=16, layers=2)
+    with pytest.raises(ValueError, match="reserved"):
+        cache.store(0, k, v)
+    for bad in (dict(k=k), dict(k=k, v=v[:-1]), dict(k=k.float(), v=v), dict(k=k[:, :1], v=v)):
+        with pytest.raises(ValueError, match="needed"):
+            pruner.step(cur, cache=cache, **bad)
+    with pytest.raises(ValueError, match="sequences"):
+        pruner.step(cur, cache=PagedCache(5, n_pages=20, max_pages=10, Hkv=2, d=64, page_size=16), k=k, v=v)
+    assert pruner.dl is dl and not cache.seq_len.any() and cache.slots is None
+    h, _, keep, *_ = pruner.step(cur, cache=cache, k=k, v=v)
+    k1, v1 = rnd(h.shape[0], 2, 64), rnd(h.shape[0], 2, 64)
+    cache.store(1, k1, v1)
+    s = cache.slots.long()
+    for layer, (a, b) in enumerate(((k[keep.long()], v[keep.long()]), (k1, v1))):
+        P = cache.layers[layer]
+        assert torch.equal(P.k[s // 16, :, s % 16], a) and torch.equal(P.v[s // 16, :, s % 16], b)
+
+
 def test_captured_decode_step():
     # reserve, store, attend, captured once and replayed while the cache grows past page borders
     Hq, Hkv, d, B, page, scale = 28, 4, 128, 5, 16, 128 ** -0.5
