@@ -391,10 +391,10 @@ typedef struct {
  *     batch).
  *   seq_len_out [B], free_count_out [1] int32 (outputs): the state afterwards.
  * A request has no place if its row of the table is too short, if its new
- * tokens reach past n_new, or (needing pages) if the pages it and the requests before it need are more than the
- * stack holds: its length and row stay as they were, its slots are -1 and it
- * flags AVTP_FLAG_NO_PAGES.  A page id outside [0, n_pages) gives slots of -1
- * and flags AVTP_FLAG_BAD_PAGE.  free_count is read as at most n_pages.
+ * tokens reach past n_new, or (needing pages) if the pages that it and the
+ * requests before it need are more than the stack holds: its length and row stay
+ * as they were, its slots are -1 and it flags AVTP_FLAG_NO_PAGES.  A page id
+ * outside [0, n_pages) gives slots of -1 and flags AVTP_FLAG_BAD_PAGE.  free_count is read as at most n_pages.
  * ---------------------------------------------------------------------- */
 int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
                      const int32_t *seq_len, const int32_t *free_pages, int n_pages,
@@ -407,8 +407,9 @@ int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *
  * request has ended; seq_len[b] or more: nothing changes; less: tokens are
  * taken back, e.g. rejected drafts).  The pages that hold none of the kept
  * tokens are pushed onto the stack, sequences in order, each one's in token
- * order; the table is only read.  seq_len_out [B] = min(keep_len, seq_len),
- * free_count_out [1].  Pages beyond the stack's n_pages entries (more pages
+ * order; the table is only read, and every page of a row counts as its
+ * sequence's own (one that two rows name is handed back twice).  seq_len_out [B]
+ * = min(keep_len, seq_len), free_count_out [1].  Pages beyond the stack's n_pages entries (more pages
  * handed back than the pool has) are dropped and flag AVTP_FLAG_OUT_CAPACITY.
  * ---------------------------------------------------------------------- */
 int avtp_page_trim(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
@@ -455,7 +456,9 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * maxima are fp32.  A block table entry outside [0, n_pages) reads nothing: its
  * tokens count as zeros and flag AVTP_FLAG_BAD_PAGE; so does a kv_len above
  * max_pages * page_size, of which the tokens in the table remain; a negative
- * one is 0.  No atomics on results: reruns are bit-identical.
+ * one is 0.  No atomics on results: reruns are bit-identical.  The running sums
+ * refer to a maximum that may lag by 2^16, so |v| of 2^100 and more may overflow
+ * where the formula's quotient does not; a row whose logits are all -inf gives 0.
  * ws: device scratch of avtp_page_attention_workspace_size() bytes (which may
  * be 0, and is for an invalid argument), 256-byte aligned, no initialisation;
  * it depends on the sizes alone, so that a call captured at the largest
