@@ -394,7 +394,8 @@ typedef struct {
  * tokens reach past n_new, or (needing pages) if the pages that it and the
  * requests before it need are more than the stack holds: its length and row stay
  * as they were, its slots are -1 and it flags AVTP_FLAG_NO_PAGES.  A page id
- * outside [0, n_pages) gives slots of -1 and flags AVTP_FLAG_BAD_PAGE.  free_count is read as at most n_pages.
+ * outside [0, n_pages) gives slots of -1 and flags AVTP_FLAG_BAD_PAGE.
+ * free_count is read as at most n_pages.
  * ---------------------------------------------------------------------- */
 int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
                      const int32_t *seq_len, const int32_t *free_pages, int n_pages,
@@ -409,8 +410,9 @@ int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *
  * tokens are pushed onto the stack, sequences in order, each one's in token
  * order; the table is only read, and every page of a row counts as its
  * sequence's own (one that two rows name is handed back twice).  seq_len_out [B]
- * = min(keep_len, seq_len), free_count_out [1].  Pages beyond the stack's n_pages entries (more pages
- * handed back than the pool has) are dropped and flag AVTP_FLAG_OUT_CAPACITY.
+ * = min(keep_len, seq_len), free_count_out [1].  Pages beyond the stack's
+ * n_pages entries (more pages handed back than the pool has) are dropped and
+ * flag AVTP_FLAG_OUT_CAPACITY.
  * ---------------------------------------------------------------------- */
 int avtp_page_trim(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
                    const int32_t *seq_len, const int32_t *block_table, int max_pages,
