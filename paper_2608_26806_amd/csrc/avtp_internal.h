@@ -148,7 +148,8 @@ struct PageAttnPlan {
   bool brief;      // few rows and keys: a block per tile, nothing cut
   int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
   int nsplit;      // many: key ranges per tile
-  int least;       // few: units (32 keys of a tile) per worker, many: keys per range, at least
+  int least;       // few: units (32 keys of a tile) per worker, at least
+  float gain, from;  // many: a tile's key ranges (key_ranges)
   int cuts;        // tiles that may have been cut, and how many parts they may leave:
   size_t off_lse, off_meta, bytes;  // rows fp32, their log2 sums, whose they are
 };

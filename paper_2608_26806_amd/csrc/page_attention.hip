@@ -88,6 +88,7 @@ struct KArgs {
   int32_t *status;
   int B, Hq, Hkv, G, N_q, max_pages, n_pages, page_shift;
   int workers, nsplit, least;  // see PageAttnPlan
+  float gain, from;
   int4 *meta;                  // two per possible cut tile
   float cl2e;
 };
@@ -856,6 +857,22 @@ __global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(KArgs
   }
 }
 
+// Ranges of a tile's keys.  bf16: cut into r of them, a tile's S stages take 1/r of
+// their time, but its parts are written, read and joined, t(r) = stage S / r + part T r
+// + join with T tiles: least at r = sqrt(gain S), gain = stage / (part T), and worth it
+// where r (r - 2) > join / (part T), which is r > from.  28/4 heads of 128, prompt of
+// 1,000 tokens 31.8 -> 27.4 us against ranges of 256 keys, of 300 16.5 -> 12.8; 32/8
+// heads, 500 tokens 20.5 -> 16.7, four chunks of 30 over 3,000 keys 28.9 -> 26.1.
+// fp32 (gain 0), whose stages take 5 times as long: ranges of 64 keys (by the formula
+// two prompts of 700 tokens, 14/2 heads of 64, 43 -> 45-52).
+template <int KS>
+__host__ __device__ inline int key_ranges(int keys, float gain, float from) {
+  if (gain == 0.f) return (keys + 63) / 64;
+  const int stages = (keys + KS - 1) / KS;
+  const float r = sqrtf(gain * (float)stages);
+  return r <= from ? 1 : r < (float)stages ? (int)(r + 0.5f) : stages;
+}
+
 // Many rows per sequence (chunks of tokens): a block takes one tile of 128 rows
 // of one key head, or one of nsplit ranges of its keys where there are few
 // tiles.  The tiles of one sequence go together, key heads fastest, so that
@@ -877,9 +894,10 @@ __global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void
   Cut c{};
   if (tile >= 0) {
     const int keys = tile_keys<BM>(a, s, tile);
-    // whole stages, evenly; a range has `least` keys or more
+    // whole stages, evenly
     const int stages = max(1, (keys + KS - 1) / KS);
-    const int ranges = min(a.nsplit, max(1, (keys + a.least - 1) / a.least)), each = (stages + ranges - 1) / ranges;
+    const int ranges = min(a.nsplit, max(1, key_ranges<KS>(keys, a.gain, a.from)));
+    const int each = (stages + ranges - 1) / ranges;
     const int parts = (stages + each - 1) / each;
     if (split >= parts) return;
     const Job job{g, b, tile * BM, split * each * KS, min(keys, (split + 1) * each * KS), place * a.nsplit + split,
@@ -1018,15 +1036,18 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     L.cuts = (int)L.blocks;
     slots = 2 * L.blocks;
   } else {
-    // Two blocks per CU, of 256 keys or more.  In fp32, whose products take 16
-    // times as long, four (two of 512-byte rows) of 64 or more: one chunk of 1,000
-    // tokens, 16/8 heads of 128, 85 us with half as many, 70 with these, 88 with
-    // twice as many.  (bf16 with twice as many: four chunks of 300 tokens 20 -> 31.)
+    // Two blocks per CU.  In fp32 four (two of 512-byte rows): one chunk of 1,000
+    // tokens, 16/8 heads of 128, 85 us with half as many, 70 with these, 88 with twice
+    // as many.  (bf16 with twice as many: four chunks of 300 tokens 20 -> 31.)
     const bool f32 = P.dtype == AVTP_FP32;
     const int64_t want = f32 && P.d == 64 ? 1024 : 512;
-    L.least = f32 ? 64 : 256;
-    const int64_t most = (max_kv_len + L.least - 1) / L.least;
-    const int64_t ns = tiles < 1 ? 1 : want / tiles;
+    // us: a stage of 64 keys, a part written and read, the second launch
+    const float part = 0.04f * P.d / 128 * tiles, join = 4.f;
+    if (!f32) L.gain = (P.d == 64 ? 0.7f : 1.1f) / part;
+    L.from = 1 + std::sqrt(1 + join / part);
+    const int most = many_tiles(P.d * (f32 ? 4 : 2)) == 1 ? key_ranges<kTile>(max_kv_len, L.gain, L.from)
+                                                          : key_ranges<2 * kTile>(max_kv_len, L.gain, L.from);
+    const int64_t ns = want / tiles;
     L.nsplit = (int)(ns < 1 ? 1 : ns < most ? ns : most);
     L.blocks = tiles * L.nsplit;
     L.cuts = L.nsplit > 1 ? (int)tiles : 0;
@@ -1097,6 +1118,8 @@ hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const Page
   k.workers = (int)L.blocks;
   k.nsplit = L.nsplit;
   k.least = L.least;
+  k.gain = L.gain;
+  k.from = L.from;
   k.cl2e = A.scale * kLog2e;
   if (P.dtype == AVTP_FP32) return P.d == 64 ? launch<float, 64>(st, L, k) : launch<float, 128>(st, L, k);
   return P.d == 64 ? launch<__bf16, 64>(st, L, k) : launch<__bf16, 128>(st, L, k);
