@@ -143,9 +143,9 @@ hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void
 // Attention over the pages: its launch, from host-known sizes only (so the
 // workspace size and the launch always agree).
 struct PageAttnPlan {
-  bool few;        // few rows per sequence: one wave has them all
+  bool few;        // tiles of one wave's rows
   int tile;        // rows of a tile: 16 or 32 (few), 128
-  bool brief;      // few rows and keys: a block per tile, nothing cut
+  bool brief;      // short work: a block per tile, nothing cut
   int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
   int nsplit;      // many: key ranges per tile
   int least;       // few: units (32 keys of a tile) per worker, at least

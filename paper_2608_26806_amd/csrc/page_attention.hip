@@ -809,7 +809,7 @@ __device__ inline int tile_of_rank(const KArgs &a, int rank, int &b, Seq &s) {
   return tile < tiles_of<BM>(a, s) ? tile : -1;
 }
 
-// Few rows and few keys: a block takes a whole tile, its W waves a share of the
+// Short work: a block takes a whole tile, its W waves a share of the
 // keys each, and joins their parts in LDS: no second launch.
 constexpr int kShortWaves = 4;  // whose buffers a CU's LDS holds
 template <typename T, int D, int M>
@@ -989,13 +989,22 @@ __global__ __launch_bounds__(kJoinThreads) void page_join_kernel(KArgs a) {
 }
 
 constexpr int kManyWaves = 4;
-// Few rows and few keys in bf16: a block per tile that joins its waves' parts
-// itself, while the tiles fit on the chip at once (320 for 32 requests of 8 key
-// heads) and four waves are enough for a tile's keys.  One request, 28/4 heads of
-// 128: 793 keys 10.3 -> 8.9 us, 1,500 keys 12.0 -> 12.6; 32 requests of 300 keys,
-// 32/8 heads, 16.2 -> 12.7, 64 of them 19.9 -> 31.3.  fp32 keeps the line: 8 requests
-// of 300 keys 16.6 -> 19.3.
-constexpr int kShortTiles = 384, kShortKeys = 1024;
+// Short work in bf16: a block per tile of 16 or 32 rows that joins its waves' parts
+// itself, while the tiles fit on the chip at once (of 512-byte parts one on a CU, of
+// 256-byte ones two; the bound counts up to a tile too many per sequence) and four
+// waves are enough for a tile's keys.
+// One token, 28/4 heads of 128: 793 keys 10.3 -> 8.9 us, 1,500 keys 10.7 -> 12.6; 32
+// requests of 300 keys, 32/8 heads, 16.2 -> 12.7, 64 of them 19.9 -> 31.3; 28 of 900,
+// 16/16 heads of 64, 24.3 -> 19.0.  Prompts against blocks of 128 rows: 200 tokens, 28/4
+// heads 12.1 -> 8.9 us, two of 200, 32/8 heads (416 tiles) 11.8 -> 13.9, of 400, 16/16
+// heads of 64 (432) 11.4 -> 9.1, four of 300 (656) 10.3 -> 12.6.
+// Twice the keys where the tiles fill half of the chip, since ranges of keys gain less
+// there: eight chunks of 30 over 1,500 keys, 32/8 heads (304 tiles) 36.3 -> 22.3 us,
+// over 3,000 37.3 -> 35.8, two of 60 over 3,500 (136) 25.9 -> 33.5; one of 30 over 1,500,
+// 28/4 heads (28) 15.9 -> 18.8.  Not for single tokens, whose sequences differ most in
+// length (60 of 10-2,000 keys 18.9 -> 25.6).
+// fp32 keeps the line: 8 requests of 300 keys 16.6 -> 19.3.
+constexpr int kShortTiles = 384, kShortTiles64 = 512, kShortKeys = 1024, kShortFull = 128, kShortFullKeys = 2048;
 // 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
 constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
@@ -1006,12 +1015,15 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // (longer sequences run all the same)
   max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
   const int64_t rows = N_q * (Hq / P.Hkv);
-  // one wave of 16 or 32 rows for a sequence, or blocks of 128
-  L.few = rows <= (int64_t)B * 32;
-  const int bm = L.tile = rows <= (int64_t)B * 16 ? 16 : L.few ? 32 : kManyWaves * 32;
-  // (at most: the ranks that the kernels give them)
-  const int64_t tiles = (rows / bm + B) * P.Hkv;
-  L.brief = L.few && P.dtype == AVTP_BF16 && tiles <= kShortTiles && max_kv_len <= kShortKeys;
+  // one wave of 16 or 32 rows for a sequence, or blocks of 128; a tile's ranks: at most
+  auto tiles_of = [&](int bm) { return (rows / bm + B) * P.Hkv; };
+  const int small = rows <= (int64_t)B * 16 ? 16 : 32;
+  const int64_t brief = tiles_of(small);
+  L.brief = P.dtype == AVTP_BF16 && brief <= (P.d == 64 ? kShortTiles64 : kShortTiles) &&
+            max_kv_len <= (small == 32 && brief >= kShortFull ? kShortFullKeys : kShortKeys);
+  L.few = L.brief || rows <= (int64_t)B * 32;
+  const int bm = L.tile = L.few ? small : kManyWaves * 32;
+  const int64_t tiles = tiles_of(bm);
   int64_t slots;
   if (L.brief) {
     L.blocks = tiles;

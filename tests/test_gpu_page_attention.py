@@ -394,3 +394,25 @@ def test_first_row_is_not_row_zero():
         m = n * B
         assert torch.equal(moved[150:150 + m], out[:m]) and torch.equal(mlse[:, 150:150 + m], lse[:, :m])
         assert (moved[:150] == 7.0).all() and (moved[150 + m:] == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype, Hq, Hkv, d", KINDS)
+def test_chunks_in_every_form(dtype, Hq, Hkv, d):
+    # short chunks as tiles of one block each (bf16), and with a bound that spreads them over blocks of 128 rows
+    # and key ranges; tiles without keys, tiles of a few rows, more sequences than a wave has lanes
+    for new, kv in (([1, 3, 0, 33, 130, 2], [1, 70, 40, 33, 200, 300]), ([70, 5, 130, 1], [300, 900, 130, 1]),
+                    ([60, 60], [1000, 20]), ([12] * 66 + [0, 0, 40], [12 + 5 * i for i in range(66)] + [0, 90, 0])):
+        c = Case(sum(new) + Hq, dtype, Hq, Hkv, d, 32, new, kv)
+        ref = c.oracle()
+        c.check(c.run(), ref)
+        c.check(c.run(max_kv=1 << 20), ref)
+        assert not c.status.any()
+
+
+def test_chunks_over_bad_pages_in_every_form():
+    c = Case(24, torch.bfloat16, 4, 2, 128, 16, [100, 40, 1], [200, 90, 64])
+    c.table[0, 3], c.table[1, 0], c.table[0, 12] = -1, c.pages.n_pages, 2 ** 31 - 1
+    for bound in (200, 4096):
+        c.status.zero_()
+        c.check(c.run(max_kv=bound))
+        assert c.status.tolist() == [A.FLAG_BAD_PAGE, A.FLAG_BAD_PAGE, 0]
