@@ -1033,7 +1033,9 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     // more: a worker's time grows with its units, the join's with their number, so
     // their root.  28/4 heads, one token over 3,000 keys 14.9 -> 12.2 us against
     // single units, 10,000 21.9 -> 17.8, 40,000 35.2 -> 30.5 (a third of the root
-    // instead of a quarter: 13.1, 17.7, 29.7; a half: 13.8, 18.3, 29.9).
+    // instead of a quarter: 13.1, 17.7, 29.7; a half: 13.8, 18.3, 29.9).  A half for
+    // tiles of 32 rows, whose parts are more to join: 16/8 heads, 15 tokens over 3,000
+    // keys 19.8 -> 19.7, 10,000 30.2 -> 26.3, 40,000 55.8 -> 50.0.
     auto per_cu = [&](auto m_tag) {
       constexpr int M = decltype(m_tag)::value;
       if (P.dtype == AVTP_FP32) return P.d == 64 ? Shape<float, 64, M, 1, 1>::kPerCu : Shape<float, 128, M, 1, 1>::kPerCu;
@@ -1041,7 +1043,7 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     };
     const int64_t most = 256 * (bm == 16 ? per_cu(std::integral_constant<int, 16>{}) : per_cu(std::integral_constant<int, 32>{}));
     const int64_t units = (max_kv_len + kTile - 1) / kTile;
-    L.least = (int)(std::sqrt((double)units) / 4);
+    L.least = (int)(std::sqrt((double)units) / (bm == 16 ? 4 : 2));
     if (L.least < 1) L.least = 1;
     const int64_t need = (tiles * units + L.least - 1) / L.least;
     L.blocks = need < most ? need : most;
