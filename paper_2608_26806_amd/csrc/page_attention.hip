@@ -86,7 +86,7 @@ struct KArgs {
   float *lse, *po, *pl;
   const int32_t *cu_q, *kv_len, *table;
   int32_t *status;
-  int B, Hq, Hkv, G, N_q, max_pages, n_pages, page_shift;
+  int B, Hkv, G, N_q, max_pages, n_pages, page_shift;
   int workers, nsplit, least;  // see PageAttnPlan
   float gain, from;
   int4 *meta;                  // two per possible cut tile
@@ -1122,7 +1122,6 @@ hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const Page
   k.table = A.table;
   k.status = A.status;
   k.B = A.B;
-  k.Hq = A.Hq;
   k.Hkv = P.Hkv;
   k.G = A.Hq / P.Hkv;
   k.N_q = A.N_q;
