@@ -755,17 +755,21 @@ def page_trim(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor, blo
     return seq_len_out, free_count_out
 
 
+def page_store_rows(pages: Pages, k: torch.Tensor, v: torch.Tensor):
+    """Every check of a store's rows; returns their pointers and token strides."""
+    if k.shape != v.shape:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    return *_page_rows(k, "k", pages.Hkv, pages), *_page_rows(v, "v", pages.Hkv, pages)
+
+
 def prepare_page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot_map: torch.Tensor,
                        keep_idx: Optional[torch.Tensor] = None, stream=None) -> Prepared:
     """avtp_page_store on fixed buffers, as a Prepared call: one row for each
     entry of slot_map."""
     n = slot_map.numel()
-    if k.shape != v.shape:
-        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} differ")
+    kp, ks, vp, vs = page_store_rows(pages, k, v)
     if keep_idx is None and k.shape[0] < n:
         raise ValueError(f"slot_map has {n} entries, k and v {k.shape[0]} rows")
-    kp, ks = _page_rows(k, "k", pages.Hkv, pages)
-    vp, vs = _page_rows(v, "v", pages.Hkv, pages)
     args = (_stream(stream), pages.ref(), kp, ks, vp, vs, k.shape[0], _page_arg(slot_map, "slot_map"),
             _page_arg(keep_idx, "keep_idx", n), n)
     return Prepared(lib().avtp_page_store, args, "avtp_page_store",

@@ -70,6 +70,7 @@ class ProgressivePruner:
                 if t is None or tuple(t.shape) != want or t.dtype != pages.dtype:
                     raise ValueError(f"{name}: {list(want)} of {pages.dtype} is needed, got "
                                      f"{t if t is None else (list(t.shape), t.dtype)}")
+            A.page_store_rows(pages, k, v)  # (device, strides, alignment)
             if cache.seq_len.numel() != dl.B:
                 raise ValueError(f"the cache has {cache.seq_len.numel()} sequences, the batch {dl.B}")
         scores, isum = A.score_variation(dl, h_cur, self.h_prior, status=status)

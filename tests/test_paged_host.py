@@ -1,0 +1,62 @@
+"""The host side of the paged cache's callers, on the CPU: what a pruning step
+checks before it reserves."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2608_26806_amd import avtp as A
+from paper_2608_26806_amd.progressive import ProgressivePruner
+from paper_2608_26806_amd.workloads import build_layout
+
+
+class Cache:
+    """Stands for a PagedCache of two sequences; reserving is an error here."""
+
+    def __init__(self):
+        self.layers = [SimpleNamespace(Hkv=2, d=64, dtype=torch.bfloat16)]
+        self.seq_len = torch.zeros(2, dtype=torch.int32)
+
+    def reserve(self, *args, **kw):
+        raise AssertionError("reserved before the rows were checked")
+
+    def store(self, *args, **kw):
+        pass
+
+
+def _layouts_of_rows(n):
+    """Rows [n, 2, 64] that no store takes, and the refusal."""
+    flat = torch.zeros(n * 136 + 8, dtype=torch.bfloat16)
+    return {
+        "head-major": (torch.zeros(2, n, 64, dtype=torch.bfloat16).transpose(0, 1), "contiguous"),
+        "value-major": (torch.zeros(n, 64, 2, dtype=torch.bfloat16).transpose(1, 2), "contiguous"),
+        "one row for all": (torch.zeros(1, 2, 64, dtype=torch.bfloat16).expand(n, 2, 64), "overlap"),
+        "a stride of 132": (flat[:n * 132].view(n, 132)[:, :128].unflatten(1, (2, 64)), "aligned"),
+        "four values off": (flat[4:4 + n * 136].view(n, 136)[:, :128].unflatten(1, (2, 64)), "aligned"),
+    }
+
+
+@pytest.mark.parametrize("which", sorted(_layouts_of_rows(3)))
+@pytest.mark.parametrize("name", ["k", "v"])
+def test_a_pruning_step_checks_the_layout_of_k_and_v_before_it_reserves(monkeypatch, which, name):
+    dl = A.DeviceLayout(build_layout([[9, 7], [5]], 2, 4, 50), host_only=True)
+    monkeypatch.setattr(A, "_page_arg", lambda *args: 0)          # (the rows are in host memory)
+    monkeypatch.setattr(A, "score_variation", lambda *args, **kw: (None, None))
+    monkeypatch.setattr(A, "budget_select_compact", lambda *args, **kw: (None, None, None))
+    good = torch.zeros(dl.N_tok, 2, 64, dtype=torch.bfloat16)
+    bad, match = _layouts_of_rows(dl.N_tok)[which]
+    kv = {"k": good, "v": good, name: bad}
+    h = torch.zeros(dl.N_tok, 8)
+    pruner = ProgressivePruner(dl, h)
+    with pytest.raises(ValueError, match=f"{name}: .*{match}"):
+        pruner.step(h, cache=Cache(), **kv)
+    assert pruner.dl is dl
+
+
+def test_a_pruning_step_refuses_rows_in_host_memory_before_it_reserves(monkeypatch):
+    dl = A.DeviceLayout(build_layout([[9, 7], [5]], 2, 4, 50), host_only=True)
+    monkeypatch.setattr(A, "score_variation", lambda *args, **kw: (None, None))
+    monkeypatch.setattr(A, "budget_select_compact", lambda *args, **kw: (None, None, None))
+    h, k = torch.zeros(dl.N_tok, 8), torch.zeros(dl.N_tok, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(ValueError, match="k: a GPU tensor"):
+        ProgressivePruner(dl, h).step(h, cache=Cache(), k=k, v=k)
