@@ -81,3 +81,14 @@ class PagedCache:
         A.prepare_page_trim(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
                             self.free_count, self._after[:B], self._after[B:], status)()
         self._state.copy_(self._after)
+
+    def _mark(self):
+        """What ``_take_back`` needs to undo the reservations that follow."""
+        return self.seq_len.clone(), self.slots
+
+    def _take_back(self, mark) -> None:
+        """Undo what was reserved since ``mark`` was made: the lengths are as they were
+        and the pages are free again (the ones taken last on top of the stack)."""
+        seq_len, slots = mark
+        self.trim(seq_len)
+        self.slots = slots

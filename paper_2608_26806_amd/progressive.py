@@ -57,7 +57,10 @@ class ProgressivePruner:
         takes the kept rows of the layer's k and v [N_tok, Hkv, d] behind what
         its sequences hold already, into the pages of its layer ``layer``; the
         layers up to the next pruning one store theirs in the same slots
-        (``cache.store(layer + 1, k, v)``, of the kept tokens).
+        (``cache.store(layer + 1, k, v)``, of the kept tokens).  Sequences
+        that get no pages flag FLAG_NO_PAGES in ``status`` [B] and their rows are
+        in no page; without a status the step raises, and then (as after any
+        failure) the cache holds what it held before.
         Returns (h_out, [compacted others], keep_idx, budget, scores, img_sum);
         afterwards self.dl is the next layer's layout (keep totals from
         keep_pct_next) and self.h_prior is h_out."""
@@ -81,10 +84,22 @@ class ProgressivePruner:
             pairs.append((src, torch.empty(shape, dtype=src.dtype, device=src.device), tdim))
         bud, keep, cu_out = A.budget_select_compact(dl, isum, scores, pairs, self.alpha, self.lo, self.hi,
                                                     self.floor, mode=self.mode, status=status)
-        if cache is not None:
-            cache.store(layer, k, v, cache.reserve(cu_out, dl.N_out, status=status), keep_idx=keep)
-        # (one synchronisation per pruning layer)
-        self.dl = A.DeviceLayout.pruned(dl, keep, cu_out,
-                                        lambda n, cu: keep_totals(n, cu, keep_pct_next))
+        mark = None if cache is None else cache._mark()
+        try:
+            if cache is not None:
+                flags = torch.zeros(dl.B, dtype=torch.int32, device=h_cur.device) if status is None else status
+                cache.store(layer, k, v, cache.reserve(cu_out, dl.N_out, status=flags), keep_idx=keep)
+            # (one synchronisation per pruning layer)
+            following = A.DeviceLayout.pruned(dl, keep, cu_out,
+                                              lambda n, cu: keep_totals(n, cu, keep_pct_next))
+            if cache is not None and status is None:
+                short = [b for b, f in enumerate(flags.tolist()) if f]
+                if short:
+                    raise RuntimeError(f"no pages for the kept tokens of sequences {short}")
+        except Exception:
+            if cache is not None:
+                cache._take_back(mark)
+            raise
+        self.dl = following
         self.h_prior = pairs[0][1]
         return pairs[0][1], [p[1] for p in pairs[1:]], keep, bud, scores, isum
