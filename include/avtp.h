@@ -396,12 +396,22 @@ typedef struct {
  * as they were, its slots are -1 and it flags AVTP_FLAG_NO_PAGES.  A page id
  * outside [0, n_pages) gives slots of -1 and flags AVTP_FLAG_BAD_PAGE.
  * free_count is read as at most n_pages.
+ * avtp_page_reserve is the same call with one more output, kv_len_out [B]: the
+ * lengths for avtp_page_attention, which counts a sequence's queries back from
+ * its length and would take those of a request without a place for its last
+ * cached tokens.  It is seq_len_out, but 0 for such a request, whose queries then
+ * see nothing (out 0, lse -inf).
  * ---------------------------------------------------------------------- */
 int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
                      const int32_t *seq_len, const int32_t *free_pages, int n_pages,
                      const int32_t *free_count, int32_t *block_table, int max_pages,
                      int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
                      int32_t *free_count_out, int32_t *status);
+int avtp_page_reserve(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
+                      const int32_t *seq_len, const int32_t *free_pages, int n_pages,
+                      const int32_t *free_count, int32_t *block_table, int max_pages,
+                      int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
+                      int32_t *free_count_out, int32_t *kv_len_out, int32_t *status);
 
 /* ------------------------------------------------------------------------
  * avtp_page_trim -- sequences are cut to their first keep_len[b] tokens (0: the
@@ -437,7 +447,8 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
 /* ------------------------------------------------------------------------
  * avtp_page_attention -- the attention of a chunk of new tokens over the
  * paged cache, their own K and V included.  The queries of sequence b are rows
- * cu_q[b] .. cu_q[b+1]-1 of q, its last n_b = cu_q[b+1] - cu_q[b] tokens; row t
+ * cu_q[b] .. cu_q[b+1]-1 of q, its last n_b = cu_q[b+1] - cu_q[b] tokens (which
+ * must be in the cache: avtp_page_reserve for requests without a place); row t
  * of them sees the first kv_len[b] - n_b + t + 1 cached tokens.  With c =
  * softmax_scale and query head h using key head g = h / (Hq/Hkv):
  *   lse[h,t] = log sum_j exp(c q_{t,h}.k_{j,g}),

@@ -95,6 +95,8 @@ def lib() -> ctypes.CDLL:
         i64, PP = ctypes.c_int64, ctypes.POINTER(_Pages)
         L.avtp_page_tables.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, vp, c_int, vp, i64,
                                        vp, vp, vp]
+        L.avtp_page_reserve.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, vp, c_int, vp, i64,
+                                        vp, vp, vp, vp]
         L.avtp_page_trim.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, c_int, vp, vp, vp, vp]
         L.avtp_page_store.argtypes = [vp, PP, vp, i64, vp, i64, i64, vp, vp, i64]
         L.avtp_page_attention_workspace_size.argtypes = [PP, c_int, c_int, i64, i64]
@@ -108,7 +110,7 @@ def lib() -> ctypes.CDLL:
                   "avtp_compact",
                   "avtp_layer_attention", "avtp_layer_select", "avtp_pruned_layout",
                   "avtp_select_compact", "avtp_budget_select_compact", "avtp_page_tables",
-                  "avtp_page_trim", "avtp_page_store", "avtp_page_attention"):
+                  "avtp_page_reserve", "avtp_page_trim", "avtp_page_store", "avtp_page_attention"):
             getattr(L, f).restype = c_int
         _lib = L
     return _lib
@@ -695,8 +697,9 @@ def prepare_page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Ten
                         free_pages: torch.Tensor, free_count: torch.Tensor,
                         block_table: torch.Tensor, slot_map: torch.Tensor, seq_len_out: torch.Tensor,
                         free_count_out: torch.Tensor, status: Optional[torch.Tensor] = None,
-                        stream=None) -> Prepared:
-    """avtp_page_tables on fixed buffers, as a Prepared call."""
+                        stream=None, kv_len_out: Optional[torch.Tensor] = None) -> Prepared:
+    """avtp_page_tables (avtp_page_reserve with a kv_len_out) on fixed buffers, as a
+    Prepared call."""
     B = seq_len.numel()
     _check_table(block_table, B)
     args = (_stream(stream), B, int(page_size), _page_arg(cu_new, "cu_new", B + 1),
@@ -704,11 +707,14 @@ def prepare_page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Ten
             free_pages.numel(), _page_arg(free_count, "free_count", 1),
             _page_arg(block_table, "block_table"), block_table.shape[1],
             _page_arg(slot_map, "slot_map"), slot_map.numel(),
-            _page_arg(seq_len_out, "seq_len_out", B), _page_arg(free_count_out, "free_count_out", 1),
-            _page_arg(status, "status", B))
-    return Prepared(lib().avtp_page_tables, args, "avtp_page_tables",
-                    (cu_new, seq_len, free_pages, free_count, block_table, slot_map, seq_len_out,
-                     free_count_out, status, stream))
+            _page_arg(seq_len_out, "seq_len_out", B), _page_arg(free_count_out, "free_count_out", 1))
+    keep = (cu_new, seq_len, free_pages, free_count, block_table, slot_map, seq_len_out,
+            free_count_out, kv_len_out, status, stream)
+    last = _page_arg(status, "status", B)
+    if kv_len_out is None:
+        return Prepared(lib().avtp_page_tables, (*args, last), "avtp_page_tables", keep)
+    return Prepared(lib().avtp_page_reserve, (*args, _page_arg(kv_len_out, "kv_len_out", B), last),
+                    "avtp_page_reserve", keep)
 
 
 def page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Tensor, free_pages: torch.Tensor,

@@ -14,7 +14,9 @@ stack of free pages, and each layer's pages.
 
 Every step runs in libavtp.so on torch's current stream; nothing is read back
 to the host, and the state lies in buffers that stay where they are, so the
-calls of a decode step can be captured into a graph and replayed.
+calls of a decode step can be captured into a graph and replayed.  ``seq_len``,
+``free_count``, ``block_table`` and ``free_pages`` are there to be read;
+``reserve`` and ``trim`` change them.
 """
 from __future__ import annotations
 
@@ -38,6 +40,9 @@ class PagedCache:
         # call's results over
         self._state, self._after = ints(requests + 1), ints(requests + 1)
         self.seq_len, self.free_count = self._state[:requests], self._state[requests:]
+        # the lengths as attention takes them: 0 for requests that got no place in
+        # the last reservation, so that their queries see nothing
+        self._seen = ints(requests)
         self.block_table = ints(requests, max_pages) - 1
         self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
         self.free_count.fill_(n_pages)
@@ -47,12 +52,15 @@ class PagedCache:
                 status: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Room for cu_new[b+1] - cu_new[b] more tokens of every sequence, in
         every layer; returns their slots (n_new entries, -1 where a request got
-        no place), which ``store`` takes by default."""
+        no place), which ``store`` takes by default.  A request without a place
+        keeps its length, flags FLAG_NO_PAGES in ``status`` [B], and until the
+        next reservation ``attend`` gives its queries out 0 and lse -inf."""
         if slot_map is None:
             slot_map = torch.empty(n_new, dtype=torch.int32, device=cu_new.device)
         B = self.seq_len.numel()
         A.prepare_page_tables(self.page_size, cu_new, self.seq_len, self.free_pages, self.free_count,
-                              self.block_table, slot_map, self._after[:B], self._after[B:], status)()
+                              self.block_table, slot_map, self._after[:B], self._after[B:], status,
+                              kv_len_out=self._seen)()
         self._state.copy_(self._after)
         self.slots = slot_map
         return slot_map
@@ -71,8 +79,9 @@ class PagedCache:
                lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
                ws: Optional[torch.Tensor] = None):
         """The new tokens (the last cu_q[b+1] - cu_q[b] of each sequence, whose
-        K and V are stored) over the layer's pages; returns (out, lse)."""
-        return A.page_attention(self.layers[layer], q, cu_q, self.seq_len, self.block_table,
+        K and V are stored) over the layer's pages; returns (out, lse).  Queries
+        of a request that got no place for them: out 0, lse -inf."""
+        return A.page_attention(self.layers[layer], q, cu_q, self._seen, self.block_table,
                                 softmax_scale, max_kv_len, out, lse, status, ws)
 
     def trim(self, keep_len: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
@@ -80,15 +89,16 @@ class PagedCache:
         B = self.seq_len.numel()
         A.prepare_page_trim(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
                             self.free_count, self._after[:B], self._after[B:], status)()
+        torch.minimum(self._seen, self._after[:B], out=self._seen)
         self._state.copy_(self._after)
 
     def _mark(self):
         """What ``_take_back`` needs to undo the reservations that follow."""
-        return self.seq_len.clone(), self.slots
+        return self.seq_len.clone(), self._seen.clone(), self.slots
 
     def _take_back(self, mark) -> None:
         """Undo what was reserved since ``mark`` was made: the lengths are as they were
         and the pages are free again (the ones taken last on top of the stack)."""
-        seq_len, slots = mark
+        seq_len, seen, self.slots = mark
         self.trim(seq_len)
-        self.slots = slots
+        self._seen.copy_(seen)

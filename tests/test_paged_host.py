@@ -1,5 +1,6 @@
 """The host side of the paged cache's callers, on the CPU: what a pruning step
 checks before it reserves."""
+import ctypes
 from types import SimpleNamespace
 
 import pytest
@@ -60,3 +61,19 @@ def test_a_pruning_step_refuses_rows_in_host_memory_before_it_reserves(monkeypat
     h, k = torch.zeros(dl.N_tok, 8), torch.zeros(dl.N_tok, 2, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError, match="k: a GPU tensor"):
         ProgressivePruner(dl, h).step(h, cache=Cache(), k=k, v=k)
+
+
+BUF = torch.zeros(4096, dtype=torch.uint8)          # (never dereferenced: the calls are refused)
+P, Q = ctypes.c_void_p(BUF.data_ptr()), ctypes.c_void_p(BUF.data_ptr() + 64)
+RESERVE = dict(stream=None, B=3, page_size=16, cu_new=P, seq_len=P, free_pages=P, n_pages=10, free_count=P,
+               block_table=P, max_pages=4, slot_map=P, n_new=5, seq_len_out=Q, free_count_out=Q, kv_len_out=Q,
+               status=None)
+
+
+@pytest.mark.parametrize("patch, rc", [
+    (dict(kv_len_out=None), A.ERR_INVALID_ARG), (dict(kv_len_out=P), A.ERR_INVALID_ARG),
+    (dict(seq_len_out=P), A.ERR_INVALID_ARG), (dict(free_count_out=None), A.ERR_INVALID_ARG),
+    (dict(cu_new=None), A.ERR_INVALID_ARG), (dict(B=0), A.ERR_INVALID_ARG), (dict(B=1 << 17), A.ERR_UNSUPPORTED),
+    (dict(page_size=24), A.ERR_UNSUPPORTED), (dict(n_new=-1), A.ERR_INVALID_ARG)])
+def test_reserve_refusals(patch, rc):
+    assert A.lib().avtp_page_reserve(*{**RESERVE, **patch}.values()) == rc
