@@ -685,6 +685,8 @@ class Pages:
         return cls(new(), new())
 
     def ref(self):
+        # (as for every other tensor of a call; the pages may be older than the current device)
+        _page_arg(self.k, "pages", 1, None)
         return ctypes.byref(self.st)
 
 

@@ -77,3 +77,23 @@ RESERVE = dict(stream=None, B=3, page_size=16, cu_new=P, seq_len=P, free_pages=P
     (dict(page_size=24), A.ERR_UNSUPPORTED), (dict(n_new=-1), A.ERR_INVALID_ARG)])
 def test_reserve_refusals(patch, rc):
     assert A.lib().avtp_page_reserve(*{**RESERVE, **patch}.values()) == rc
+
+
+def test_pages_on_another_device_than_the_current_one_are_refused(monkeypatch):
+    # stand-ins for tensors on the second of two devices; the launch would be on the first
+    def tensor(device):
+        return SimpleNamespace(is_cuda=True, device=torch.device("cuda", device), dtype=torch.bfloat16, shape=(4, 2, 16, 64),
+                               is_contiguous=lambda: True, numel=lambda: 8192, data_ptr=lambda: P.value, dim=lambda: 4)
+
+    current = [1]
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    pages = A.Pages(tensor(1), tensor(1))
+    assert A.page_attention_workspace_bytes(pages, 4, 1, 1, 5000) > 0
+    current[0] = 0
+    monkeypatch.setattr(A, "_page_rows", lambda t, name, heads, pages: (P, 128))    # (rows on device 0)
+    rows, slots = SimpleNamespace(shape=(3, 2, 64)), tensor(0)
+    slots.dtype, slots.numel = torch.int32, lambda: 3
+    with pytest.raises(ValueError, match="pages: on cuda:1"):
+        A.prepare_page_store(pages, rows, rows, slots, stream=ctypes.c_void_p(0))
+    with pytest.raises(ValueError, match="pages: on cuda:1"):
+        A.page_attention_workspace_bytes(pages, 4, 1, 1, 5000)
