@@ -470,8 +470,10 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * tokens count as zeros and flag AVTP_FLAG_BAD_PAGE; so does a kv_len above
  * max_pages * page_size, of which the tokens in the table remain; a negative
  * one is 0.  No atomics on results: reruns are bit-identical.  The running sums
- * refer to a maximum that may lag by 2^16, so |v| of 2^100 and more may overflow
- * where the formula's quotient does not; a row whose logits are all -inf gives 0.
+ * refer to a maximum that may lag behind, and then hold up to 2^13 for every token
+ * a row sees: |v| may be 2^114 over the number of those tokens (2^97 of 131,072);
+ * beyond it an output may overflow where the formula's quotient does not.  A row
+ * whose logits are all -inf gives 0.
  * ws: device scratch of avtp_page_attention_workspace_size() bytes (which may
  * be 0, and is for an invalid argument), 256-byte aligned, no initialisation;
  * it depends on the sizes alone, so that a call captured at the largest

@@ -47,7 +47,10 @@ constexpr int kTile = 32;  // keys of a tile
 // A row's exponentials refer to the largest logit m of some earlier tile, not
 // always of all: only when their sum over a tile leaves this range is m raised
 // (and the sum and output so far scaled).  fp32 sums, and products with bf16 or
-// fp32 probabilities of that size, are as exact as with the true maximum.
+// fp32 probabilities of that size, are as exact as with the true maximum.  The limit
+// holds for the keys of one lane, 8 of a tile's 32 at the fewest (the 16-row MFMA): a
+// row's sum stays below 2^13 per key, and its output below 2^128 while |v| is at
+// most 2^114 over the keys.
 constexpr float kLazyLimit = 65536.f;
 
 template <typename T, int D>
