@@ -57,3 +57,35 @@ def test_the_largest_values_over_a_long_cache(dtype, d, new, weight, bound):
     step = 2.0 ** -8 if dtype == torch.bfloat16 else E
     assert np.isfinite(out).all() and (np.abs(out - o) <= (2 * es + (n / 2 + 20) * E + 2.02 * step) * size).all()
     assert (np.abs(lse - x) <= es + 2.0 ** -22 * np.abs(x)).all()
+
+
+# levels that rise in the first and in the second tile of a stage of 64 keys, fall, and rise past all before
+STEPS = ((0, 0.0), (96, 20.0), (128, 3.0), (256, 45.0), (288, 10.0), (416, 70.0), (430, 5.0), (704, 90.0), (740, 60.0))
+
+
+def _rising(dtype, Hq, Hkv, d, new, kv):
+    c = Case(sum(new) + d, dtype, Hq, Hkv, d, 32, new, kv, scale=1.0)
+    c.pages.k.mul_(0.3)
+    level = np.zeros(max(kv))
+    for t, x in STEPS:
+        level[t:] = x
+    _set_level(c, level)
+    c.q.mul_(0.5)
+    # rows that rise at different steps: some hardly at all, some at each
+    c.q[..., 0] = torch.linspace(0.02, 1.4, c.q[..., 0].numel(), device="cuda").reshape(c.q.shape[:2]).to(dtype)
+    return c
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("Hq, Hkv, new, kv, bounds", [
+    (8, 2, [1] * 5, [900, 97, 257, 430, 800], (900, 4096, 1)),            # 16-row tiles: short and few, in one piece too
+    (4, 2, [12, 10, 14], [900, 300, 770], (900, 4096, 1)),                # 32-row tiles: short and few
+    (4, 2, [70, 3], [900, 500], (900, 4096, 1)),                          # mixed, blocks of 128 rows in ranges
+    (4, 2, [40 + i for i in range(30)], [300 + 20 * i for i in range(30)], (4096,)),   # blocks of 128 rows, uncut in bf16
+    (40, 1, [1, 1], [900, 440], (900, 4096, 1))])                         # 40 rows of one token
+def test_rising_and_falling_maxima_in_every_form(dtype, d, Hq, Hkv, new, kv, bounds):
+    c = _rising(dtype, Hq, Hkv, d, new, kv)
+    ref = _reference(c)
+    for bound in bounds:
+        c.check(c.run(max_kv=bound), ref)
