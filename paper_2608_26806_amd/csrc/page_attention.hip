@@ -381,9 +381,10 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     const int key = min(ks + r0w + (lane & (NG - 1)) * 16, L - 1);
     return trow[key >> a.page_shift];
   };
-  // Decode steps read K and V once: non-temporal (64 requests' step 206 -> 194 us;
-  // chunks read them again, from the L2).
-  constexpr int kAux = WR == 1 ? 2 : 0;
+  // Decode steps read K and V once: non-temporal (64 requests' step 206 -> 194 us).
+  // Chunks, 32-row tiles of the short form among them, read them again, from the L2
+  // (eight of 30 tokens over 1,500 keys, 32/8 heads, 23.1 us non-temporal, 20.9 so).
+  constexpr int kAux = WR == 1 && !(HERE && M == 32) ? 2 : 0;
   auto issue = [&](AVTP_LDS char *buf, int ks, int ids) __attribute__((always_inline)) {
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
