@@ -462,7 +462,8 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  *   lse     [Hq, N_q] fp32, natural log (may be NULL): the row_lse of
  *     avtp_score for the text rows of the layer;
  *   max_kv_len: a bound on kv_len, which sizes the launch and the workspace
- *     only (with a lower one the results are the same, slower).
+ *     only.  Any value is right for all lengths; the speed is best with one
+ *     near the longest (see Speed).
  * A single new token per sequence is the decode step.  Products of bf16 run on
  * the bf16 MFMA with fp32 accumulation, the probabilities rounded to bf16 before
  * they weigh V (2^-8 of each at most); fp32 runs in fp32.  Sums and
@@ -481,8 +482,13 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * need one each.  N_q * Hq is below 2^31, Hq at most 256, and with more than 32
  * rows per sequence N_q * Hq / 128 + B * Hkv below 2^24.
  * Speed: with at most 32 rows (tokens times Hq / Hkv) per sequence on average,
- * the call is bound by reading K and V once; with more, by the products.  A batch of
- * long chunks and single tokens is best issued as two calls.
+ * the call is bound by reading K and V once; with more, by the products, or by its
+ * longest sequence where many differ much in length (64 of 300 to 16,000 tokens, 7
+ * query heads per key head: 4 new tokens each 102 us, 5 of them 294).  A batch of
+ * long chunks and single tokens is best issued as two calls.  A max_kv_len below the
+ * lengths makes too few blocks; one far above them costs steps of few or short
+ * requests time (one token over 794: 9 us up to 1,024, 16 at 32,768, 22 at 131,072;
+ * 64 requests of 300 tokens 21 and 31; of 300 to 16,000 163 and 169).
  * ---------------------------------------------------------------------- */
 size_t avtp_page_attention_workspace_size(const avtp_pages *pages, int Hq, int B, int64_t N_q,
                                           int64_t max_kv_len);

@@ -5,8 +5,9 @@
 // m to m' its sum and its output so far are scaled by exp(m - m').  Neither the
 // logits nor the probabilities leave the registers:
 //   S^T = K Q^T: keys are the MFMA's rows, query rows its columns, so a lane
-//     owns one query row (half of its keys; the other half is 32 lanes away)
-//     and the softmax needs one exchange per tile, for the maximum;
+//     owns one query row (half of its keys with the 32-row MFMA, the other half
+//     is 32 lanes away; with the 16-row MFMA a quarter, 16 lanes apart) and the
+//     softmax needs one exchange per tile, for the maximum;
 //   O^T = V^T P^T: the probabilities a lane holds are its part of the second
 //     product's operand as they are (the order of the keys inside a product is
 //     free, as long as V's rows come in the same order), and scaling O by
@@ -154,14 +155,14 @@ struct Mma<16> {
 
 // The work.  A row tile is BM rows (token, head of the group) of one sequence
 // and key head; a unit is one stage of KS keys of a tile, and a tile has the
-// units of the keys its last row sees (one at least).  All units stand in one
-// line, key head by key head, sequence by sequence, tile by tile, and every
-// worker (block) takes the same number of them, so that long and short
-// sequences, causal tiles and few rows alike keep all of the chip busy to the
-// end.  A worker finds its first unit from the lengths alone.  A tile that the
-// line cuts leaves parts in the workspace, which page_join_kernel joins.  (With
-// one block per tile and key range, eight requests' chunks over 1,000 to 12,000
-// keys took 473 us, 64 requests' decode step 214.)
+// units of the keys its last row sees (one at least).  With few rows per sequence
+// all units stand in one line, key head by key head, sequence by sequence, tile by
+// tile, and every worker (block) takes the same number of them, so that long and
+// short sequences keep all of the chip busy to the end (64 requests' decode step
+// 162 us; a block per tile and key range 214).  A worker finds its first unit from
+// the lengths alone.  A tile that the line cuts leaves parts in the workspace,
+// which page_join_kernel joins.  With many rows, and in short work, a block takes a
+// tile or a range of its keys (page_attn_many_kernel, page_attn_short_kernel).
 struct Seq {
   int q0, n, kv, L;  // first row, new tokens, cached tokens, those the table has room for
 };
@@ -507,7 +508,11 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     }
     return S;
   };
-  // p = 2^(c S - m), as the second product takes them, and their sum
+  // p = 2^(c S - m), as the second product takes them, and their sum.  In bf16 they
+  // are rounded to it (2^-8 of each at most), since the bf16 MFMA takes V as it is
+  // only beside bf16 and p as a sum of two bf16 parts would double these products;
+  // their sum is that of the fp32 values.  The output's error against 64 bits, relative
+  // 2-norm, is 0.0019-0.0022 instead of the 0.0016-0.0017 of an output in bf16 alone.
   struct Probs {
     std::conditional_t<F32, float, bf16x8> x[F32 ? NE : NE / 8];
   };
@@ -865,7 +870,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(KArgs
 // their time, but its parts are written, read and joined, t(r) = stage S / r + part T r
 // + join with T tiles: least at r = sqrt(gain S), gain = stage / (part T), and worth it
 // where r (r - 2) > join / (part T), which is r > from.  28/4 heads of 128, prompt of
-// 1,000 tokens 31.8 -> 27.4 us against ranges of 256 keys, of 300 16.5 -> 12.8; 32/8
+// 1,000 tokens 31.8 -> 26.6 us against ranges of 256 keys, of 300 16.5 -> 12.4; 32/8
 // heads, 500 tokens 20.5 -> 16.7, four chunks of 30 over 3,000 keys 28.9 -> 26.1.
 // fp32 (gain 0), whose stages take 5 times as long: ranges of 64 keys (by the formula
 // two prompts of 700 tokens, 14/2 heads of 64, 43 -> 45-52).
@@ -997,16 +1002,16 @@ constexpr int kManyWaves = 4;
 // itself, while the tiles fit on the chip at once (of 512-byte parts one on a CU, of
 // 256-byte ones two; the bound counts up to a tile too many per sequence) and four
 // waves are enough for a tile's keys.
-// One token, 28/4 heads of 128: 793 keys 10.3 -> 8.9 us, 1,500 keys 10.7 -> 12.6; 32
-// requests of 300 keys, 32/8 heads, 16.2 -> 12.7, 64 of them 19.9 -> 31.3; 28 of 900,
-// 16/16 heads of 64, 24.3 -> 19.0.  Prompts against blocks of 128 rows: 200 tokens, 28/4
-// heads 12.1 -> 8.9 us, two of 200, 32/8 heads (416 tiles) 11.8 -> 13.9, of 400, 16/16
-// heads of 64 (432) 11.4 -> 9.1, four of 300 (656) 10.3 -> 12.6.
+// One token, 28/4 heads of 128: 794 keys 10.2 -> 8.9 us, 1,500 keys 11.7 -> 16.9; 32
+// requests of 300 keys, 32/8 heads, 17.1 -> 15.0, 64 of them 21.4 -> 33.6; 28 of 900,
+// 16/16 heads of 64, 26.1 -> 20.4.  Prompts against blocks of 128 rows: 200 tokens, 28/4
+// heads 12.3 -> 8.9 us, two of 200, 32/8 heads (416 tiles) 11.7 -> 13.9, 400, 16/16
+// heads of 64 (416) 11.3 -> 7.3, two of 300 9.9 -> 8.2, four (656) 10.3 -> 12.6.
 // Twice the keys where the tiles fill half of the chip, since ranges of keys gain less
-// there: eight chunks of 30 over 1,500 keys, 32/8 heads (304 tiles) 36.3 -> 22.3 us,
-// over 3,000 37.3 -> 35.8, two of 60 over 3,500 (136) 25.9 -> 33.5; one of 30 over 1,500,
-// 28/4 heads (28) 15.9 -> 18.8.  Not for single tokens, whose sequences differ most in
-// length (60 of 10-2,000 keys 18.9 -> 25.6).
+// there: eight chunks of 30 over 1,500 keys, 32/8 heads (304 tiles) 37.7 -> 21.2 us,
+// over 3,000 40.8 -> 37.0, two of 60 over 3,500 (136) 25.3 -> 32.0; one of 30 over 1,500,
+// 28/4 heads (28) 16.6 -> 17.8.  Not for single tokens, whose sequences differ most in
+// length (60 of 10-2,000 keys, 28/4 heads, 19.8 -> 27.2).
 // fp32 keeps the line: 8 requests of 300 keys 16.6 -> 19.3.
 constexpr int kShortTiles = 384, kShortTiles64 = 512, kShortKeys = 1024, kShortFull = 128, kShortFullKeys = 2048;
 // 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
@@ -1025,6 +1030,13 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   const int64_t brief = tiles_of(small);
   L.brief = P.dtype == AVTP_BF16 && brief <= (P.d == 64 ? kShortTiles64 : kShortTiles) &&
             max_kv_len <= (small == 32 && brief >= kShortFull ? kShortFullKeys : kShortKeys);
+  // Up to 32 rows a sequence is one tile of the even line; more rows read its keys once
+  // per 32 there and once per 128 in a block.  us, line against blocks: 28/4 heads, 64
+  // requests of 300-16,000 keys, 4 tokens (28 rows) 102 / 292, 5 (35 rows) 183 / 294, 9 (63)
+  // 190 / 296, 18 (126) 362 / 296; eight of them, 28 rows 28.8 / 29.8, 35 rows 38.2 / 29.9; 32/8
+  // heads, eight of 3,000 keys, 32 rows 34.0 / 32.4, 36 rows 43.1 / 34.1; one of 10,000,
+  // 28/4 heads, 28 rows 24.8 / 19.4.  (It loses for 33 to 64 rows of many sequences of very
+  // different length, and for 17 to 32 rows of a single long one.)
   L.few = L.brief || rows <= (int64_t)B * 32;
   const int bm = L.tile = L.few ? small : kManyWaves * 32;
   const int64_t tiles = tiles_of(bm);
@@ -1035,11 +1047,13 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   } else if (L.few) {
     // As many workers as the CUs' LDS holds, with `least` units (of 32 keys) each or
     // more: a worker's time grows with its units, the join's with their number, so
-    // their root.  28/4 heads, one token over 3,000 keys 14.9 -> 12.2 us against
-    // single units, 10,000 21.9 -> 17.8, 40,000 35.2 -> 30.5 (a third of the root
-    // instead of a quarter: 13.1, 17.7, 29.7; a half: 13.8, 18.3, 29.9).  A half for
-    // tiles of 32 rows, whose parts are more to join: 16/8 heads, 15 tokens over 3,000
-    // keys 19.8 -> 19.7, 10,000 30.2 -> 26.3, 40,000 55.8 -> 50.0.
+    // their root.  28/4 heads, one token over 3,000 keys 15.1 -> 12.8 us against
+    // single units, 10,000 22.1 -> 18.5, 40,000 36.7 -> 32.2.  Half of the root for tiles
+    // of 32 rows, whose parts are more to join: 16/8 heads, 15 tokens over 3,000 keys
+    // 25.0 -> 19.5, 10,000 36.2 -> 26.2, 40,000 51.7 -> 50.1.  The units are those of
+    // max_kv_len, so a bound far above the lengths leaves few requests fewer workers
+    // than would be best: one token over 794 keys 8.9 us at the exact bound, 16.2 at
+    // 32,768, 22.0 at 131,072; 64 requests of 300-16,000 keys 163 and 169.
     auto per_cu = [&](auto m_tag) {
       constexpr int M = decltype(m_tag)::value;
       if (P.dtype == AVTP_FP32) return P.d == 64 ? Shape<float, 64, M, 1, 1>::kPerCu : Shape<float, 128, M, 1, 1>::kPerCu;
@@ -1059,7 +1073,9 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     // as many.  (bf16 with twice as many: four chunks of 300 tokens 20 -> 31.)
     const bool f32 = P.dtype == AVTP_FP32;
     const int64_t want = f32 && P.d == 64 ? 1024 : 512;
-    // us: a stage of 64 keys, a part written and read, the second launch
+    // us: a stage of 64 keys, a part written and read, the second launch (tiles of 64 rows
+    // over 1,024 and 4,096 keys, 8-256 of them: a stage 1.09 at d 128, 0.77 at d 64; a fit over
+    // one to 16 ranges gives 0.041 and 0.029 a part, 3.5 and 1.8 for the launch)
     const float part = 0.04f * P.d / 128 * tiles, join = 4.f;
     if (!f32) L.gain = (P.d == 64 ? 0.7f : 1.1f) / part;
     L.from = 1 + std::sqrt(1 + join / part);
