@@ -475,7 +475,7 @@ int avtp_page_reserve(avtp_stream_t stream, int B, int page_size, const int32_t 
                       const int32_t *free_count, int32_t *block_table, int max_pages,
                       int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
                       int32_t *free_count_out, int32_t *kv_len_out, int32_t *status) {
-  if (!kv_len_out) return AVTP_ERR_INVALID_ARG;
+  if (!kv_len_out || kv_len_out == seq_len_out) return AVTP_ERR_INVALID_ARG;
   return page_tables(stream, B, page_size, cu_new, seq_len, free_pages, n_pages, free_count, block_table,
                      max_pages, slot_map, n_new, seq_len_out, free_count_out, kv_len_out, status);
 }
