@@ -12,11 +12,12 @@ stack of free pages, and each layer's pages.
     out, lse = cache.attend(layer, q, cu_q, scale)     # new tokens over the cache
     cache.trim(keep_len)                               # requests that ended, drafts taken back
 
-Every step runs in libavtp.so on torch's current stream; nothing is read back
-to the host, and the state lies in buffers that stay where they are, so the
-calls of a decode step can be captured into a graph and replayed.  ``seq_len``,
-``free_count``, ``block_table`` and ``free_pages`` are there to be read;
-``reserve`` and ``trim`` change them.
+Every step runs in libavtp.so on torch's current stream (torch copies the new
+lengths over the old ones); nothing is read back to the host, and the state
+lies in buffers that stay where they are, so the calls of a decode step can be
+captured into a graph and replayed.  ``seq_len``, ``free_count``,
+``block_table`` and ``free_pages`` are there to be read; ``reserve`` and
+``trim`` change them.
 """
 from __future__ import annotations
 
