@@ -396,11 +396,13 @@ typedef struct {
  * as they were, its slots are -1 and it flags AVTP_FLAG_NO_PAGES.  A page id
  * outside [0, n_pages) gives slots of -1 and flags AVTP_FLAG_BAD_PAGE.
  * free_count is read as at most n_pages.
- * avtp_page_reserve is the same call with one more output, kv_len_out [B]: the
- * lengths for avtp_page_attention, which counts a sequence's queries back from
- * its length and would take those of a request without a place for its last
- * cached tokens.  It is seq_len_out, but 0 for such a request, whose queries then
- * see nothing (out 0, lse -inf).
+ * avtp_page_reserve is the same call and keeps kv_len [B], the lengths for
+ * avtp_page_attention, which counts a sequence's queries back from its length and
+ * would take those of a request without a place for its last cached tokens.
+ * kv_len[b] becomes seq_len_out[b], or 0 for a request without a place, whose
+ * queries then see nothing (out 0, lse -inf); sequences without new tokens keep
+ * theirs, so that a refusal stands until the request gets its place.  (Behind
+ * avtp_page_trim: the smaller of kv_len and its seq_len_out.)
  * ---------------------------------------------------------------------- */
 int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
                      const int32_t *seq_len, const int32_t *free_pages, int n_pages,
@@ -411,7 +413,7 @@ int avtp_page_reserve(avtp_stream_t stream, int B, int page_size, const int32_t 
                       const int32_t *seq_len, const int32_t *free_pages, int n_pages,
                       const int32_t *free_count, int32_t *block_table, int max_pages,
                       int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
-                      int32_t *free_count_out, int32_t *kv_len_out, int32_t *status);
+                      int32_t *free_count_out, int32_t *kv_len, int32_t *status);
 
 /* ------------------------------------------------------------------------
  * avtp_page_trim -- sequences are cut to their first keep_len[b] tokens (0: the

@@ -699,8 +699,8 @@ def prepare_page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Ten
                         free_pages: torch.Tensor, free_count: torch.Tensor,
                         block_table: torch.Tensor, slot_map: torch.Tensor, seq_len_out: torch.Tensor,
                         free_count_out: torch.Tensor, status: Optional[torch.Tensor] = None,
-                        stream=None, kv_len_out: Optional[torch.Tensor] = None) -> Prepared:
-    """avtp_page_tables (avtp_page_reserve with a kv_len_out) on fixed buffers, as a
+                        stream=None, kv_len: Optional[torch.Tensor] = None) -> Prepared:
+    """avtp_page_tables (avtp_page_reserve with a kv_len) on fixed buffers, as a
     Prepared call."""
     B = seq_len.numel()
     _check_table(block_table, B)
@@ -711,11 +711,11 @@ def prepare_page_tables(page_size: int, cu_new: torch.Tensor, seq_len: torch.Ten
             _page_arg(slot_map, "slot_map"), slot_map.numel(),
             _page_arg(seq_len_out, "seq_len_out", B), _page_arg(free_count_out, "free_count_out", 1))
     keep = (cu_new, seq_len, free_pages, free_count, block_table, slot_map, seq_len_out,
-            free_count_out, kv_len_out, status, stream)
+            free_count_out, kv_len, status, stream)
     last = _page_arg(status, "status", B)
-    if kv_len_out is None:
+    if kv_len is None:
         return Prepared(lib().avtp_page_tables, (*args, last), "avtp_page_tables", keep)
-    return Prepared(lib().avtp_page_reserve, (*args, _page_arg(kv_len_out, "kv_len_out", B), last),
+    return Prepared(lib().avtp_page_reserve, (*args, _page_arg(kv_len, "kv_len", B), last),
                     "avtp_page_reserve", keep)
 
 

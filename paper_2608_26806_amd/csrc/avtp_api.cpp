@@ -445,20 +445,20 @@ static int page_tables(avtp_stream_t stream, int B, int page_size, const int32_t
                        const int32_t *seq_len, const int32_t *free_pages, int n_pages,
                        const int32_t *free_count, int32_t *block_table, int max_pages,
                        int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
-                       int32_t *free_count_out, int32_t *kv_len_out, int32_t *status) {
+                       int32_t *free_count_out, int32_t *kv_len, int32_t *status) {
   int rc = check_tables(B, page_size, max_pages, n_pages);
   if (rc != AVTP_OK) return rc;
   if (!cu_new || !seq_len || !free_pages || !free_count || !block_table || !seq_len_out ||
       !free_count_out || n_new < 0 || (n_new > 0 && !slot_map))
     return AVTP_ERR_INVALID_ARG;
   // blocks read the state that another block would overwrite
-  if (seq_len_out == seq_len || free_count_out == free_count || kv_len_out == seq_len)
+  if (seq_len_out == seq_len || free_count_out == free_count || kv_len == seq_len)
     return AVTP_ERR_INVALID_ARG;
   if (n_new > INT32_MAX) return AVTP_ERR_UNSUPPORTED;
   const PageTables P{B,       __builtin_ctz((unsigned)page_size), max_pages,      n_pages, seq_len,
                      free_count, seq_len_out,                     free_count_out, status};
   return hip_status(launch_page_tables((hipStream_t)stream, P, cu_new, free_pages, block_table,
-                                       slot_map, n_new, kv_len_out));
+                                       slot_map, n_new, kv_len));
 }
 
 int avtp_page_tables(avtp_stream_t stream, int B, int page_size, const int32_t *cu_new,
@@ -474,10 +474,10 @@ int avtp_page_reserve(avtp_stream_t stream, int B, int page_size, const int32_t 
                       const int32_t *seq_len, const int32_t *free_pages, int n_pages,
                       const int32_t *free_count, int32_t *block_table, int max_pages,
                       int32_t *slot_map, int64_t n_new, int32_t *seq_len_out,
-                      int32_t *free_count_out, int32_t *kv_len_out, int32_t *status) {
-  if (!kv_len_out || kv_len_out == seq_len_out) return AVTP_ERR_INVALID_ARG;
+                      int32_t *free_count_out, int32_t *kv_len, int32_t *status) {
+  if (!kv_len || kv_len == seq_len_out) return AVTP_ERR_INVALID_ARG;
   return page_tables(stream, B, page_size, cu_new, seq_len, free_pages, n_pages, free_count, block_table,
-                     max_pages, slot_map, n_new, seq_len_out, free_count_out, kv_len_out, status);
+                     max_pages, slot_map, n_new, seq_len_out, free_count_out, kv_len, status);
 }
 
 int avtp_page_trim(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,

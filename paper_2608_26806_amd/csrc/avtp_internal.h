@@ -132,7 +132,7 @@ struct PageTables {
 };
 hipError_t launch_page_tables(hipStream_t stream, const PageTables &P, const int32_t *cu_new,
                               const int32_t *free_pages, int32_t *block_table, int32_t *slot_map,
-                              int64_t n_new, int32_t *kv_len_out);
+                              int64_t n_new, int32_t *kv_len);
 hipError_t launch_page_trim(hipStream_t stream, const PageTables &P, const int32_t *keep_len,
                             const int32_t *block_table, int32_t *free_pages);
 hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void *k,

@@ -48,7 +48,7 @@ struct Need {
 struct TArgs {
   PageTables p;
   const int32_t *cu_new, *free_pages;
-  int32_t *table, *slot_map, *kv_len_out;
+  int32_t *table, *slot_map, *kv_len;
   int n_new;
 };
 
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(kThreads) void page_tables_kernel(TArgs a) {
         if (fits && r[j].need > 0) got = off + r[j].need;  // (fitting requests are a prefix of those in need)
         if (mine) {
           a.p.seq_len_out[b] = fits ? r[j].L + r[j].n : r[j].L;
-          if (a.kv_len_out) a.kv_len_out[b] = fits ? r[j].L + r[j].n : 0;
+          if (a.kv_len && r[j].n > 0) a.kv_len[b] = fits ? r[j].L + r[j].n : 0;
           if (!fits && a.p.status) atomicOr(&a.p.status[b], AVTP_FLAG_NO_PAGES);
         }
         if (here) {
@@ -216,9 +216,9 @@ __global__ __launch_bounds__(kThreads) void page_trim_kernel(RArgs a) {
 
 hipError_t launch_page_tables(hipStream_t st, const PageTables &P, const int32_t *cu_new,
                               const int32_t *free_pages, int32_t *block_table, int32_t *slot_map,
-                              int64_t n_new, int32_t *kv_len_out) {
+                              int64_t n_new, int32_t *kv_len) {
   clear_pending_error();
-  const TArgs a{P, cu_new, free_pages, block_table, slot_map, kv_len_out, (int)n_new};
+  const TArgs a{P, cu_new, free_pages, block_table, slot_map, kv_len, (int)n_new};
   const long long nb = (n_new + kSlots - 1) / kSlots, sb = (P.B + kChunk - 1) / kChunk;
   hipLaunchKernelGGL(page_tables_kernel, dim3((unsigned)(nb > sb ? nb : sb)), dim3(kThreads), 0, st, a);
   return hipGetLastError();

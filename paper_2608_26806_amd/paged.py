@@ -41,8 +41,8 @@ class PagedCache:
         # call's results over
         self._state, self._after = ints(requests + 1), ints(requests + 1)
         self.seq_len, self.free_count = self._state[:requests], self._state[requests:]
-        # the lengths as attention takes them: 0 for requests that got no place in
-        # the last reservation, so that their queries see nothing
+        # the lengths as attention takes them: 0 for requests whose last new tokens
+        # got no place, so that their queries see nothing
         self._seen = ints(requests)
         self.block_table = ints(requests, max_pages) - 1
         self.free_pages = torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device)
@@ -54,14 +54,14 @@ class PagedCache:
         """Room for cu_new[b+1] - cu_new[b] more tokens of every sequence, in
         every layer; returns their slots (n_new entries, -1 where a request got
         no place), which ``store`` takes by default.  A request without a place
-        keeps its length, flags FLAG_NO_PAGES in ``status`` [B], and until the
-        next reservation ``attend`` gives its queries out 0 and lse -inf."""
+        keeps its length, flags FLAG_NO_PAGES in ``status`` [B], and until a
+        reservation gives it one ``attend`` gives its queries out 0 and lse -inf."""
         if slot_map is None:
             slot_map = torch.empty(n_new, dtype=torch.int32, device=cu_new.device)
         B = self.seq_len.numel()
         A.prepare_page_tables(self.page_size, cu_new, self.seq_len, self.free_pages, self.free_count,
                               self.block_table, slot_map, self._after[:B], self._after[B:], status,
-                              kv_len_out=self._seen)()
+                              kv_len=self._seen)()
         self._state.copy_(self._after)
         self.slots = slot_map
         return slot_map

@@ -109,7 +109,8 @@ def test_a_pruning_step_that_fails_behind_the_reservation_takes_its_places_back(
 
 @pytest.mark.parametrize("B, high, free", [(1, 40, 9), (5, 300, 20), (64, 1, 30), (1500, 60, 2000), (3000, 1, 40)])
 def test_lengths_for_attention(B, high, free):
-    # the outputs of the call without them, and 0 for the requests without a place (rows too short, pages, slots)
+    # the outputs of the call without them; 0 for the requests without a place (rows too short, pages, slots), as they
+    # were for sequences without new tokens
     rng = np.random.default_rng(B)
     lens, new = rng.integers(0, 90, B), rng.integers(0, high + 1, B)
     cu = np.concatenate(([0], np.cumsum(new)))
@@ -120,11 +121,11 @@ def test_lengths_for_attention(B, high, free):
         t, status, n_new = ints(table), ints([0] * B), max(0, int(cu[-1]) - 3)
         slots, out, left = ints([5] * n_new), ints([5] * B), ints([5])
         A.prepare_page_tables(16, ints(cu), ints(lens), ints(range(free)), ints([free]), t, slots, out, left, status,
-                              kv_len_out=kv)()
+                              kv_len=kv)()
         got.append([x.tolist() for x in (t, status, slots, out, left)])
     assert got[0] == got[1]
     flags, out = got[0][1], got[0][3]
-    assert kv.tolist() == [0 if f & A.FLAG_NO_PAGES else n for f, n in zip(flags, out)] + [-7]
+    assert kv.tolist() == [(0 if f & A.FLAG_NO_PAGES else n) if x else -7 for f, n, x in zip(flags, out, new)] + [-7]
     assert B == 1 or any(flags)
 
 
@@ -209,3 +210,23 @@ def test_a_captured_step_runs_into_a_shortage_and_out_of_it():
             _check_rows(out[b:b + 1], lse[:, b:b + 1], ks[b], vs[b], q[b:b + 1], [len(ks[b])], scale)
         assert cache.seq_len.tolist() == [len(x) for x in ks]
     assert refused == 6                                             # request 0 four times, request 1 twice
+
+
+def test_a_reservation_for_others_does_not_lift_a_refusal():
+    # two reservations (say prompts, then single tokens) before one attention over both
+    rnd, scale = _normal(13), 0.125
+    cache = PagedCache(3, n_pages=4, max_pages=4, Hkv=2, d=64, page_size=16)
+    say("[paged steps] two reservations, the first with a refusal")
+    _, k0, v0 = _rows(rnd, 33)
+    cache.store(0, k0, v0, cache.reserve(ints([0, 16, 32, 33]), 33))
+    q, k, v = _rows(rnd, 41)
+    status = torch.zeros(3, dtype=torch.int32, device="cuda")
+    cache.store(0, k[:40], v[:40], cache.reserve(ints([0, 0, 40, 40]), 40, status=status))
+    cache.store(0, k[40:], v[40:], cache.reserve(ints([0, 0, 0, 1]), 1, status=status))
+    assert status.tolist() == [0, A.FLAG_NO_PAGES, 0] and cache.seq_len.tolist() == [16, 16, 2]
+    out, lse = cache.attend(0, q, ints([0, 0, 40, 41]), scale)
+    assert not out[:40].any() and (lse[:, :40] == -float("inf")).all()
+    _check_rows(out[40:], lse[:, 40:], torch.cat([k0[32:], k[40:]]), torch.cat([v0[32:], v[40:]]), q[40:], [2], scale)
+    # the untouched sequence's cached tokens are still seen
+    out, lse = cache.attend(0, q[:1], ints([0, 1, 1, 1]), scale)
+    _check_rows(out, lse, k0[:16], v0[:16], q[:1], [16], scale)

@@ -66,13 +66,13 @@ def test_a_pruning_step_refuses_rows_in_host_memory_before_it_reserves(monkeypat
 BUF = torch.zeros(4096, dtype=torch.uint8)          # (never dereferenced: the calls are refused)
 P, Q, R = (ctypes.c_void_p(BUF.data_ptr() + 64 * i) for i in range(3))
 RESERVE = dict(stream=None, B=3, page_size=16, cu_new=P, seq_len=P, free_pages=P, n_pages=10, free_count=P,
-               block_table=P, max_pages=4, slot_map=P, n_new=5, seq_len_out=Q, free_count_out=Q, kv_len_out=R,
+               block_table=P, max_pages=4, slot_map=P, n_new=5, seq_len_out=Q, free_count_out=Q, kv_len=R,
                status=None)
 
 
 @pytest.mark.parametrize("patch, rc", [
-    (dict(kv_len_out=None), A.ERR_INVALID_ARG), (dict(kv_len_out=P), A.ERR_INVALID_ARG),
-    (dict(kv_len_out=Q), A.ERR_INVALID_ARG),
+    (dict(kv_len=None), A.ERR_INVALID_ARG), (dict(kv_len=P), A.ERR_INVALID_ARG),
+    (dict(kv_len=Q), A.ERR_INVALID_ARG),
     (dict(seq_len_out=P), A.ERR_INVALID_ARG), (dict(free_count_out=None), A.ERR_INVALID_ARG),
     (dict(cu_new=None), A.ERR_INVALID_ARG), (dict(B=0), A.ERR_INVALID_ARG), (dict(B=1 << 17), A.ERR_UNSUPPORTED),
     (dict(page_size=24), A.ERR_UNSUPPORTED), (dict(n_new=-1), A.ERR_INVALID_ARG)])
