@@ -65,7 +65,9 @@ typedef enum {
 #define AVTP_FLAG_OUT_CAPACITY 8    /* kept list longer than keep_capacity (truncated), */
                                     /* or a full page stack (avtp_page_trim)            */
 #define AVTP_FLAG_BAD_PAGE 16       /* a block table entry in use lies outside the pool */
-#define AVTP_FLAG_NO_PAGES 32       /* avtp_page_tables: a request got no place         */
+#define AVTP_FLAG_NO_PAGES 32       /* avtp_page_tables, _fork: a request got no place  */
+#define AVTP_FLAG_REFUSED 64        /* avtp_page_fork, avtp_page_release: the sequence  */
+                                    /* could not be forked or cut so, and stays         */
 
 /* Limits checked on the host (AVTP_ERR_UNSUPPORTED beyond them). */
 #define AVTP_MAX_IMAGES_PER_SEQ 256
@@ -75,6 +77,7 @@ typedef enum {
 #define AVTP_MAX_LAYERS 1024       /* avtp_layer_select: layers               */
 #define AVTP_MAX_SAMPLES (1 << 20) /* avtp_layer_select: samples              */
 #define AVTP_MAX_REQUESTS (1 << 16) /* avtp_page_*: sequences of a batch      */
+#define AVTP_MAX_PLANES 4          /* planes of positions of a rotation       */
 /* The attention score (avtp_score in attention mode, avtp_row_lse) addresses
  * one sequence's keys and text-row queries with 32-bit byte offsets: every
  * sequence must have (its tokens) * Hkv * d * elem and (its text rows) *
@@ -499,6 +502,127 @@ int avtp_page_attention(avtp_stream_t stream, const avtp_pages *pages, const voi
                         const int32_t *kv_len, const int32_t *block_table, int max_pages,
                         int64_t max_kv_len, float softmax_scale, void *out, int64_t out_stride,
                         float *lse, int32_t *status, void *ws, size_t ws_bytes);
+
+/* ------------------------------------------------------------------------
+ * avtp_page_attention_window -- avtp_page_attention where a row sees a window of the
+ * latest tokens and the first ones only: the token at position p (row t of sequence b:
+ * p = kv_len[b] - n_b + t) sees the cached tokens j <= p with j > p - window or
+ * j < sinks.  window is 1 or more (1: itself), sinks 0 or more.  Everything else as
+ * there, the speed's rules with the tokens that a row sees in the place of kv_len.
+ * Pages of which no row of the call sees a token are not looked at: what the table
+ * says of them does not matter (avtp_page_release hands them back).  The workspace
+ * depends on window and sinks too.
+ * ---------------------------------------------------------------------- */
+size_t avtp_page_attention_window_workspace_size(const avtp_pages *pages, int Hq, int B,
+                                                 int64_t N_q, int64_t max_kv_len, int window,
+                                                 int sinks);
+int avtp_page_attention_window(avtp_stream_t stream, const avtp_pages *pages, const void *q,
+                               int64_t q_stride, int Hq, int B, int64_t N_q, const int32_t *cu_q,
+                               const int32_t *kv_len, const int32_t *block_table, int max_pages,
+                               int64_t max_kv_len, int window, int sinks, float softmax_scale,
+                               void *out, int64_t out_stride, float *lse, int32_t *status,
+                               void *ws, size_t ws_bytes);
+
+/* ------------------------------------------------------------------------
+ * avtp_page_fork -- sequences that start from the tokens of others, e.g. more
+ * questions about the same images.  Sequence b with parent[b] = p >= 0 gets the
+ * first fork_len[b] tokens of sequence p: the pages that they fill are named by both
+ * rows from then on, and a last one that they fill in part is replaced, in b's row,
+ * by a page off the stack, dst_page[b], into which src_page[b] has to be copied in
+ * every layer (avtp_page_copy; both are -1 where there is nothing to copy).  So
+ * tokens that either sequence gets later lie in pages of its own.
+ *   parent [B]: -1 where nothing happens; sequence b must be empty, p no fork of the
+ *     same call, 0 <= fork_len[b] <= seq_len[p], and all of it where p has left tokens
+ *     behind its window (gone[p] > 0): else b stays as it was and flags
+ *     AVTP_FLAG_REFUSED.
+ *   gone, gone_out [B] (both or neither): avtp_page_release's; a fork has its parent's.
+ *   seq_len_out [B], free_count_out [1], src_page, dst_page [B] (outputs).
+ * Pages are taken in the order of the sequences; one for which none is left stays as
+ * it was and flags AVTP_FLAG_NO_PAGES (its later ones that need none are made).
+ * Behind forks sequences are cut and ended with avtp_page_release: avtp_page_trim
+ * would hand a shared page back twice.
+ *
+ * avtp_page_copy -- pages src_page[i] of a layer's K and V copied to dst_page[i], for
+ * every i < n with both inside the pool.  No page may be named as a destination and
+ * again as a source or a destination.  Bit-exact.
+ *
+ * avtp_page_release -- sequences are cut to their first keep_len[b] tokens as by
+ * avtp_page_trim (0: the request has ended), and with window > 0 they let go of the
+ * pages whose tokens have left the window: gone_out[b] = keep - window + 1 (at least
+ * gone[b]; 0 for one that has ended), and the pages of a row between those that hold
+ * the first `sinks` tokens and page gone_out[b] / page_size are no longer its own,
+ * whatever its entries say.  With no window gone may be NULL (nothing has left), or
+ * is taken over.  A page goes onto the stack when no sequence holds it any more; the
+ * pages freed by a call are pushed in ascending order.  Pages beyond the stack's
+ * n_pages entries are dropped.
+ *   A cut inside a page that another sequence held before the call would let it write
+ *   into the other's tokens, and one to less than gone[b] + window - 1 tokens would
+ *   leave tokens that have left the window missing: the sequence stays whole and flags
+ *   AVTP_FLAG_REFUSED.  (Fork the tokens to be kept to an empty row, and end this one.)
+ *   seq_len_out [B], free_count_out [1], gone_out [B] (with gone).  A block table entry
+ *   in use outside the pool is left out and flags AVTP_FLAG_BAD_PAGE.
+ * window is at most 2^30, sinks at most 2^30, and the same at every call.  ws: device
+ * scratch of avtp_page_release_workspace_size(n_pages) bytes, 256-byte aligned, no
+ * initialisation; calls that may run at the same time need one each.
+ * ---------------------------------------------------------------------- */
+int avtp_page_fork(avtp_stream_t stream, int B, int page_size, const int32_t *parent,
+                   const int32_t *fork_len, const int32_t *seq_len, const int32_t *free_pages,
+                   int n_pages, const int32_t *free_count, int32_t *block_table, int max_pages,
+                   const int32_t *gone, int32_t *seq_len_out, int32_t *free_count_out,
+                   int32_t *src_page, int32_t *dst_page, int32_t *gone_out, int32_t *status);
+int avtp_page_copy(avtp_stream_t stream, const avtp_pages *pages, const int32_t *src_page,
+                   const int32_t *dst_page, int64_t n);
+size_t avtp_page_release_workspace_size(int n_pages);
+int avtp_page_release(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
+                      const int32_t *seq_len, const int32_t *block_table, int max_pages,
+                      int32_t *free_pages, int n_pages, const int32_t *free_count, int window,
+                      int sinks, const int32_t *gone, int32_t *seq_len_out,
+                      int32_t *free_count_out, int32_t *gone_out, int32_t *status, void *ws,
+                      size_t ws_bytes);
+
+/* ------------------------------------------------------------------------
+ * avtp_norm_rotary -- queries and keys normalised head by head and rotated by
+ * their tokens' positions, in one pass.  Of the d values x of a head
+ *   y = x w / sqrt(mean(x^2) + eps)     (q_weight, k_weight [d] fp32; NULL: y = x)
+ * and of the first rot_dim of them (a multiple of 16, at most d; the others stay y)
+ * the pairs (a, b) = (y[i], y[i + rot_dim / 2]), or (y[2i], y[2i+1]) where
+ * interleaved is not 0, with t = 2 pi turns[i] / 2^64 pos[plane[i], token], become
+ *   scale (a cos t - b sin t),  scale (b cos t + a sin t).
+ * turns [rot_dim/2]: what one position turns pair i by, 2^64 a whole turn, so that
+ * positions of any size lose nothing (64-bit product, whole turns drop out); a
+ * negative frequency wraps and turns back.  Any stretching of the frequencies for
+ * long contexts is in turns and scale.  pos [planes, n] int64 (pos_stride from one
+ * plane to the next): the position ids that avtp_compact leaves; plane [rot_dim/2]
+ * names the plane of each pair (NULL: the first for all; an entry outside
+ * [0, planes) counts as 0).  planes is at most AVTP_MAX_PLANES.
+ * q, q_out [n, Hq, d], k, k_out [n, Hkv, d], d in {64, 128}; strides in elements from
+ * one token to the next (slices of a fused projection are read in place), rows and
+ * strides 16-byte aligned.  Hq or Hkv may be 0.  q_out may be q and k_out k, with the
+ * same stride.  fp32 throughout, rounded once: a square sum above 2^128 (values of
+ * about 2^60) is infinite, and gives zeros.  Infinities and NaN go through the formula.
+ * avtp_page_store_rotary is the same for the rows of a step, with K and, as they are,
+ * the rows of v on into the pages: row r to slot_map[r] (a slot outside the pool
+ * stores nothing; of two rows with one slot either may stay).  q_out is written for
+ * every row.
+ * ---------------------------------------------------------------------- */
+typedef struct {
+  const uint64_t *turns; /* device */
+  const int32_t *plane;  /* device, may be NULL */
+  int32_t rot_dim, interleaved, planes;
+  float scale;
+} avtp_rotary;
+
+int avtp_norm_rotary(avtp_stream_t stream, const avtp_rotary *rotary, int dtype, int d, int64_t n,
+                     const int64_t *pos, int64_t pos_stride, const float *q_weight,
+                     const float *k_weight, float eps, const void *q, int64_t q_stride, int Hq,
+                     void *q_out, int64_t q_out_stride, const void *k, int64_t k_stride, int Hkv,
+                     void *k_out, int64_t k_out_stride);
+int avtp_page_store_rotary(avtp_stream_t stream, const avtp_pages *pages, const avtp_rotary *rotary,
+                           int64_t n, const int64_t *pos, int64_t pos_stride,
+                           const float *q_weight, const float *k_weight, float eps, const void *q,
+                           int64_t q_stride, int Hq, void *q_out, int64_t q_out_stride,
+                           const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                           const int32_t *slot_map);
 
 /* Human-readable name of an avtp_status value (static string). */
 const char *avtp_status_string(int status);

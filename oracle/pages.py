@@ -113,3 +113,114 @@ def page_attention(k_pages, v_pages, q, cu_q, kv_len, block_table, scale):
                     weight[r, h] = (e / total) @ np.abs(vv)
                     reach[h, r] = (scale * (np.abs(kk) @ np.abs(qq))).max()
     return out, lse, (weight, reach)
+
+
+def page_attention_window(k_pages, v_pages, q, cu_q, kv_len, block_table, scale, window, sinks):
+    """``page_attention`` where the token at position p sees the tokens j <= p with
+    j > p - window or j < sinks, one by one."""
+    N, Hq, d = q.shape
+    Hkv, ps = k_pages.shape[1], k_pages.shape[2]
+    G = Hq // Hkv
+    out, lse = np.full((N, Hq, d), np.nan), np.full((Hq, N), np.nan)
+    weight, reach = np.zeros((N, Hq, d)), np.zeros((Hq, N))
+    with np.errstate(all="ignore"):
+        for b in range(len(kv_len)):
+            n = int(cu_q[b + 1] - cu_q[b])
+            held = min(int(kv_len[b]), block_table.shape[1] * ps)
+            for t in range(n):
+                p, r = int(kv_len[b]) - n + t, int(cu_q[b]) + t
+                seen = [j for j in range(0, min(p + 1, held)) if j > p - window or j < sinks]
+                out[r], lse[:, r] = 0.0, -np.inf
+                if not seen:
+                    continue
+                rows = [(int(block_table[b, j // ps]), j % ps) for j in seen]
+                none = np.zeros((Hkv, d))
+                k = np.stack([k_pages[i, :, w] if 0 <= i < len(k_pages) else none for i, w in rows]).astype(np.float64)
+                v = np.stack([v_pages[i, :, w] if 0 <= i < len(v_pages) else none for i, w in rows]).astype(np.float64)
+                for h in range(Hq):
+                    kk, vv, qq = k[:, h // G], v[:, h // G], q[r, h].astype(np.float64)
+                    z = scale * (kk @ qq)
+                    e = np.exp(z - z.max())
+                    p_ = e / e.sum()
+                    out[r, h], lse[h, r] = p_ @ vv, z.max() + np.log(e.sum())
+                    weight[r, h] = p_ @ np.abs(vv)
+                    reach[h, r] = (scale * (np.abs(kk) @ np.abs(qq))).max()
+    return out, lse, (weight, reach)
+
+
+FLAG_REFUSED = 64
+
+
+def page_fork(page_size, parent, fork_len, seq_len, free_pages, free_count, block_table, gone=None):
+    """-> (block_table, seq_len_out, free_count_out, src, dst, gone_out, flags)"""
+    n_pages, B = len(free_pages), len(seq_len)
+    table = np.array(block_table, dtype=np.int64)
+    stack = [int(x) for x in free_pages[:min(free_count, n_pages)]]
+    lens, left = np.array(seq_len, dtype=np.int64), None if gone is None else np.array(gone, dtype=np.int64)
+    src, dst, flags = np.full(B, -1), np.full(B, -1), np.zeros(B, dtype=np.int64)
+    for b in range(B):
+        p, n = int(parent[b]), int(fork_len[b])
+        if p < 0:
+            continue
+        if p >= B or parent[p] >= 0 or seq_len[b] > 0 or not 0 <= n <= seq_len[p] \
+                or -(-n // page_size) > table.shape[1] or (gone is not None and gone[p] > 0 and n != seq_len[p]):
+            flags[b] |= FLAG_REFUSED
+            continue
+        if n % page_size and not stack:
+            flags[b] |= FLAG_NO_PAGES
+            continue
+        whole = n // page_size
+        table[b, :whole] = table[p, :whole]
+        if n % page_size:
+            a, c = int(table[p, whole]), stack.pop()
+            table[b, whole] = c
+            if 0 <= a < n_pages and 0 <= c < n_pages:
+                src[b], dst[b] = a, c
+            else:
+                flags[b] |= FLAG_BAD_PAGE
+        lens[b] = n
+        if gone is not None:
+            left[b] = gone[p]
+    return table, lens, len(stack), src, dst, left, flags
+
+
+def page_copy(pages, src, dst):
+    out = np.array(pages)
+    for a, b in zip(src, dst):
+        if 0 <= a < len(out) and 0 <= b < len(out):
+            out[b] = pages[a]
+    return out
+
+
+def page_release(page_size, keep_len, seq_len, block_table, free_pages, free_count, window=0, sinks=0, gone=None):
+    """-> (free_pages, seq_len_out, free_count_out, gone_out, flags)"""
+    n_pages, B, block_table = len(free_pages), len(seq_len), np.asarray(block_table)
+    left = np.zeros(B, dtype=np.int64) if gone is None else np.array(gone, dtype=np.int64)
+    lens, flags = np.array(seq_len, dtype=np.int64), np.zeros(B, dtype=np.int64)
+
+    def entries(b, tokens, hole):
+        first = -(-sinks // page_size)
+        places = [j for j in range(-(-tokens // page_size)) if j < first or j >= hole // page_size]
+        return [int(block_table[b, j]) for j in places if j < block_table.shape[1]]
+
+    before = [entries(b, int(seq_len[b]), int(left[b])) for b in range(B)]
+    for b in range(B):
+        if any(not 0 <= i < n_pages for i in before[b]):
+            flags[b] |= FLAG_BAD_PAGE
+    holders = [i for row in before for i in row]
+    for b in range(B):
+        L, g = int(seq_len[b]), int(left[b])
+        keep = min(max(0, int(keep_len[b])), L)
+        if 0 < keep < L:
+            page = int(block_table[b, keep // page_size]) if keep % page_size else -1
+            if (0 <= page < n_pages and holders.count(page) > 1) or (g > 0 and (window == 0 or keep - window + 1 < g)):
+                flags[b] |= FLAG_REFUSED
+                continue
+        lens[b] = keep
+        left[b] = 0 if keep == 0 else max(g, keep - window + 1) if window else g
+    after = {i for b in range(B) for i in entries(b, int(lens[b]), int(left[b]))}
+    stack = [int(x) for x in free_pages[:min(free_count, n_pages)]]
+    stack += sorted({i for i in holders if 0 <= i < n_pages and i not in after})
+    out = np.array(free_pages, dtype=np.int64)
+    out[:min(len(stack), n_pages)] = stack[:n_pages]
+    return out, lens, min(len(stack), n_pages), left, flags

@@ -26,9 +26,10 @@ BF16, FP32 = 0, 1
 SCORE_ATTN, SCORE_VARIATION = 0, 1
 BUDGET_PROPORTIONAL, BUDGET_RAW = 0, 1
 FLAG_NAN_SCORE, FLAG_NO_TEXT_AFTER, FLAG_INFEASIBLE, FLAG_OUT_CAPACITY = 1, 2, 4, 8
-FLAG_BAD_PAGE, FLAG_NO_PAGES = 16, 32
+FLAG_BAD_PAGE, FLAG_NO_PAGES, FLAG_REFUSED = 16, 32, 64
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_INFEASIBLE, ERR_WORKSPACE, ERR_HIP = 0, -1, -2, -3, -4, -5
 NOALLOC_MAX_WORKSPACE = 16 << 20   # AVTP_NOALLOC_MAX_WORKSPACE of include/avtp.h
+MAX_PLANES = 4                     # AVTP_MAX_PLANES
 
 _i32p = ctypes.POINTER(ctypes.c_int32)
 
@@ -53,6 +54,12 @@ class _Tensor(ctypes.Structure):
 class _Pages(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
                [(n, ctypes.c_int32) for n in ("dtype", "n_pages", "page_size", "Hkv", "d")]
+
+
+class _Rotary(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("plane", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int32) for n in ("rot_dim", "interleaved", "planes")] + \
+               [("scale", ctypes.c_float)]
 
 
 class AvtpError(RuntimeError):
@@ -103,6 +110,22 @@ def lib() -> ctypes.CDLL:
         L.avtp_page_attention_workspace_size.restype = sz
         L.avtp_page_attention.argtypes = [vp, PP, vp, i64, c_int, c_int, i64, vp, vp, vp, c_int, i64,
                                           c_float, vp, i64, vp, vp, vp, sz]
+        L.avtp_page_attention_window_workspace_size.argtypes = [PP, c_int, c_int, i64, i64, c_int, c_int]
+        L.avtp_page_attention_window_workspace_size.restype = sz
+        L.avtp_page_attention_window.argtypes = [vp, PP, vp, i64, c_int, c_int, i64, vp, vp, vp, c_int, i64,
+                                                 c_int, c_int, c_float, vp, i64, vp, vp, vp, sz]
+        L.avtp_page_fork.argtypes = [vp, c_int, c_int, vp, vp, vp, vp, c_int, vp, vp, c_int, vp, vp, vp, vp,
+                                     vp, vp, vp]
+        L.avtp_page_copy.argtypes = [vp, PP, vp, vp, i64]
+        L.avtp_page_release_workspace_size.argtypes = [c_int]
+        L.avtp_page_release_workspace_size.restype = sz
+        L.avtp_page_release.argtypes = [vp, c_int, c_int, vp, vp, vp, c_int, vp, c_int, vp, c_int, c_int, vp,
+                                        vp, vp, vp, vp, vp, sz]
+        RP = ctypes.POINTER(_Rotary)
+        L.avtp_norm_rotary.argtypes = [vp, RP, c_int, c_int, i64, vp, i64, vp, vp, c_float, vp, i64, c_int,
+                                       vp, i64, vp, i64, c_int, vp, i64]
+        L.avtp_page_store_rotary.argtypes = [vp, PP, RP, i64, vp, i64, vp, vp, c_float, vp, i64, c_int, vp,
+                                             i64, vp, i64, vp, i64, vp]
         L.avtp_status_string.argtypes = [c_int]
         L.avtp_status_string.restype = ctypes.c_char_p
         L.avtp_version.restype = c_int
@@ -110,7 +133,9 @@ def lib() -> ctypes.CDLL:
                   "avtp_compact",
                   "avtp_layer_attention", "avtp_layer_select", "avtp_pruned_layout",
                   "avtp_select_compact", "avtp_budget_select_compact", "avtp_page_tables",
-                  "avtp_page_reserve", "avtp_page_trim", "avtp_page_store", "avtp_page_attention"):
+                  "avtp_page_reserve", "avtp_page_trim", "avtp_page_store", "avtp_page_attention",
+                  "avtp_page_attention_window", "avtp_page_fork", "avtp_page_copy", "avtp_page_release",
+                  "avtp_norm_rotary", "avtp_page_store_rotary"):
             getattr(L, f).restype = c_int
         _lib = L
     return _lib
@@ -791,30 +816,44 @@ def page_store(pages: Pages, k: torch.Tensor, v: torch.Tensor, slot_map: torch.T
     prepare_page_store(pages, k, v, slot_map, keep_idx, stream)()
 
 
-def page_attention_workspace_bytes(pages: Pages, Hq: int, B: int, N_q: int, max_kv_len: int) -> int:
-    return int(lib().avtp_page_attention_workspace_size(pages.ref(), Hq, B, N_q, max_kv_len))
+def page_attention_workspace_bytes(pages: Pages, Hq: int, B: int, N_q: int, max_kv_len: int,
+                                   window: Optional[int] = None, sinks: int = 0) -> int:
+    if window is None:
+        return int(lib().avtp_page_attention_workspace_size(pages.ref(), Hq, B, N_q, max_kv_len))
+    return int(lib().avtp_page_attention_window_workspace_size(pages.ref(), Hq, B, N_q, max_kv_len,
+                                                               *_window(window, sinks)))
+
+
+def _window(window: Optional[int], sinks: int):
+    """A window as the C ABI takes it (Python's numbers have no end)."""
+    return min(int(window), 1 << 30), min(int(sinks), 1 << 30)
 
 
 def prepare_page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: torch.Tensor,
                            block_table: torch.Tensor, softmax_scale: float, max_kv_len: int,
                            out: torch.Tensor, ws: Optional[torch.Tensor],
                            lse: Optional[torch.Tensor] = None,
-                           status: Optional[torch.Tensor] = None, stream=None) -> Prepared:
-    """avtp_page_attention on fixed buffers, as a Prepared call (ws may be None
-    where no workspace is needed)."""
+                           status: Optional[torch.Tensor] = None, stream=None,
+                           window: Optional[int] = None, sinks: int = 0) -> Prepared:
+    """avtp_page_attention (avtp_page_attention_window with a window) on fixed
+    buffers, as a Prepared call (ws may be None where no workspace is needed)."""
     B = kv_len.numel()
     _check_table(block_table, B)
     if q.dim() != 3 or q.shape != out.shape:
         raise ValueError(f"q and out must both be [N_q, Hq, d], got {tuple(q.shape)} and {tuple(out.shape)}")
+    if window is None and sinks:
+        raise ValueError("sinks go with a window")
     N, Hq, _ = q.shape
     qp, qs = _page_rows(q, "q", Hq, pages)
     op, os_ = _page_rows(out, "out", Hq, pages)
+    form = () if window is None else _window(window, sinks)
+    fn = "avtp_page_attention" if window is None else "avtp_page_attention_window"
     args = (_stream(stream), pages.ref(), qp, qs, Hq, B, N, _page_arg(cu_q, "cu_q", B + 1),
             _page_arg(kv_len, "kv_len", 1), _page_arg(block_table, "block_table"),
-            block_table.shape[1], int(max_kv_len), float(softmax_scale), op, os_,
+            block_table.shape[1], int(max_kv_len), *form, float(softmax_scale), op, os_,
             _page_arg(lse, "lse", Hq * N, torch.float32), _page_arg(status, "status", B),
             _page_arg(ws, "ws", 0, torch.uint8), 0 if ws is None else ws.numel())
-    return Prepared(lib().avtp_page_attention, args, "avtp_page_attention",
+    return Prepared(getattr(lib(), fn), args, fn,
                     (pages, q, cu_q, kv_len, block_table, out, lse, status, ws, stream))
 
 
@@ -822,10 +861,11 @@ def page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: to
                    block_table: torch.Tensor, softmax_scale: float, max_kv_len: Optional[int] = None,
                    out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
                    status: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None,
-                   stream=None):
+                   stream=None, window: Optional[int] = None, sinks: int = 0):
     """The attention of the last cu_q[b+1] - cu_q[b] tokens of every sequence
     over its pages; max_kv_len (the table's length by default) sizes the launch.
-    Returns (out [N_q, Hq, d], lse [Hq, N_q])."""
+    With a window each token sees itself and the window - 1 before it, and the first
+    ``sinks`` of the sequence.  Returns (out [N_q, Hq, d], lse [Hq, N_q])."""
     N, Hq, _ = q.shape
     if max_kv_len is None:
         max_kv_len = block_table.shape[-1] * pages.page_size
@@ -835,8 +875,210 @@ def page_attention(pages: Pages, q: torch.Tensor, cu_q: torch.Tensor, kv_len: to
         if lse is None:
             lse = torch.empty((Hq, N), dtype=torch.float32, device=q.device)
         if ws is None:
-            ws = alloc_workspace(page_attention_workspace_bytes(pages, Hq, kv_len.numel(), N, max_kv_len),
-                                 q.device)
+            ws = alloc_workspace(page_attention_workspace_bytes(pages, Hq, kv_len.numel(), N, max_kv_len,
+                                                                window, sinks), q.device)
     prepare_page_attention(pages, q, cu_q, kv_len, block_table, softmax_scale, max_kv_len, out, ws,
-                           lse, status, stream)()
+                           lse, status, stream, window, sinks)()
     return out, lse
+
+
+def prepare_page_fork(page_size: int, parent: torch.Tensor, fork_len: torch.Tensor, seq_len: torch.Tensor,
+                      free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor,
+                      seq_len_out: torch.Tensor, free_count_out: torch.Tensor, src_page: torch.Tensor,
+                      dst_page: torch.Tensor, gone: Optional[torch.Tensor] = None,
+                      gone_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                      stream=None) -> Prepared:
+    """avtp_page_fork on fixed buffers, as a Prepared call."""
+    B = seq_len.numel()
+    _check_table(block_table, B)
+    args = (_stream(stream), B, int(page_size), _page_arg(parent, "parent", B),
+            _page_arg(fork_len, "fork_len", B), _page_arg(seq_len, "seq_len", 1),
+            _page_arg(free_pages, "free_pages", 1), free_pages.numel(),
+            _page_arg(free_count, "free_count", 1), _page_arg(block_table, "block_table"),
+            block_table.shape[1], _page_arg(gone, "gone", B), _page_arg(seq_len_out, "seq_len_out", B),
+            _page_arg(free_count_out, "free_count_out", 1), _page_arg(src_page, "src_page", B),
+            _page_arg(dst_page, "dst_page", B), _page_arg(gone_out, "gone_out", B),
+            _page_arg(status, "status", B))
+    return Prepared(lib().avtp_page_fork, args, "avtp_page_fork",
+                    (parent, fork_len, seq_len, free_pages, free_count, block_table, seq_len_out,
+                     free_count_out, src_page, dst_page, gone, gone_out, status, stream))
+
+
+def page_fork(page_size: int, parent: torch.Tensor, fork_len: torch.Tensor, seq_len: torch.Tensor,
+              free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor,
+              status: Optional[torch.Tensor] = None, stream=None):
+    """Sequences that start from the first fork_len tokens of their parents
+    (block_table is updated in place).  Returns (seq_len_out, free_count_out,
+    src_page, dst_page); ``page_copy`` takes the last two, in every layer."""
+    new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+    B = seq_len.numel()
+    with _on(stream, seq_len.device):
+        out = new(B), new(1), new(B), new(B)
+    prepare_page_fork(page_size, parent, fork_len, seq_len, free_pages, free_count, block_table, *out,
+                      status=status, stream=stream)()
+    return out
+
+
+def prepare_page_copy(pages: Pages, src_page: torch.Tensor, dst_page: torch.Tensor, stream=None) -> Prepared:
+    """avtp_page_copy on fixed buffers, as a Prepared call."""
+    n = dst_page.numel()
+    args = (_stream(stream), pages.ref(), _page_arg(src_page, "src_page", n), _page_arg(dst_page, "dst_page"), n)
+    return Prepared(lib().avtp_page_copy, args, "avtp_page_copy", (pages, src_page, dst_page, stream))
+
+
+def page_copy(pages: Pages, src_page: torch.Tensor, dst_page: torch.Tensor, stream=None) -> None:
+    """Pages src_page of K and V copied to pages dst_page (-1: no copy)."""
+    prepare_page_copy(pages, src_page, dst_page, stream)()
+
+
+def page_release_workspace_bytes(n_pages: int) -> int:
+    return int(lib().avtp_page_release_workspace_size(n_pages))
+
+
+def prepare_page_release(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor,
+                         block_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                         seq_len_out: torch.Tensor, free_count_out: torch.Tensor, ws: torch.Tensor,
+                         window: int = 0, sinks: int = 0, gone: Optional[torch.Tensor] = None,
+                         gone_out: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                         stream=None) -> Prepared:
+    """avtp_page_release on fixed buffers, as a Prepared call."""
+    B = seq_len.numel()
+    _check_table(block_table, B)
+    args = (_stream(stream), B, int(page_size), _page_arg(keep_len, "keep_len", B),
+            _page_arg(seq_len, "seq_len", 1), _page_arg(block_table, "block_table"),
+            block_table.shape[1], _page_arg(free_pages, "free_pages", 1), free_pages.numel(),
+            _page_arg(free_count, "free_count", 1), *_window(window, sinks), _page_arg(gone, "gone", B),
+            _page_arg(seq_len_out, "seq_len_out", B), _page_arg(free_count_out, "free_count_out", 1),
+            _page_arg(gone_out, "gone_out", B), _page_arg(status, "status", B),
+            _page_arg(ws, "ws", 0, torch.uint8), ws.numel())
+    return Prepared(lib().avtp_page_release, args, "avtp_page_release",
+                    (keep_len, seq_len, block_table, free_pages, free_count, seq_len_out, free_count_out,
+                     ws, gone, gone_out, status, stream))
+
+
+def page_release(page_size: int, keep_len: torch.Tensor, seq_len: torch.Tensor, block_table: torch.Tensor,
+                 free_pages: torch.Tensor, free_count: torch.Tensor, window: int = 0, sinks: int = 0,
+                 gone: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
+                 ws: Optional[torch.Tensor] = None, stream=None):
+    """Cut every sequence to its first keep_len tokens and, with a window, let go
+    of what has left it; pages that no sequence holds any more go onto the stack
+    (free_pages is updated in place).  Returns (seq_len_out, free_count_out), and
+    gone_out where gone is given."""
+    new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
+    B = seq_len.numel()
+    with _on(stream, seq_len.device):
+        seq_len_out, free_count_out, gone_out = new(B), new(1), None if gone is None else new(B)
+        if ws is None:
+            ws = alloc_workspace(page_release_workspace_bytes(free_pages.numel()), seq_len.device)
+    prepare_page_release(page_size, keep_len, seq_len, block_table, free_pages, free_count, seq_len_out,
+                         free_count_out, ws, window, sinks, gone, gone_out, status, stream)()
+    return (seq_len_out, free_count_out) if gone is None else (seq_len_out, free_count_out, gone_out)
+
+
+# --------------------------------------------------------------------------- norm and rotation
+class _Rows:
+    """What ``_page_rows`` asks of the pages, for rows that go to none."""
+
+    def __init__(self, t: torch.Tensor):
+        self.d, self.dtype = t.shape[-1], t.dtype
+
+
+def _positions(rotary, pos: torch.Tensor, n: int):
+    """Pointer and plane stride of pos [planes, N] (or [N]), N at least n."""
+    p = pos[None] if pos.dim() == 1 else pos
+    if p.dim() != 2 or p.shape[0] < rotary.n_planes or p.shape[1] < n:
+        raise ValueError(f"pos: [{rotary.n_planes}, {n}] is needed, got {tuple(pos.shape)}")
+    if p.dtype != torch.int64:
+        raise TypeError(f"pos: {torch.int64} is needed, got {p.dtype}")
+    _page_arg(p[:0].reshape(-1), "pos", 0, None)
+    if p.numel() and (p.shape[1] > 1 and p.stride(1) != 1):
+        raise ValueError("pos: the positions of a plane must be contiguous")
+    if p.shape[0] > 1 and p.stride(0) < n:
+        raise ValueError("pos: planes overlap")
+    return ctypes.c_void_p(p.data_ptr()), p.stride(0) if p.shape[0] > 1 else p.shape[1]
+
+
+def _norm_weight(w: Optional[torch.Tensor], name: str, d: int):
+    if w is not None and w.numel() != d:
+        raise ValueError(f"{name}: [{d}] is needed, got {tuple(w.shape)}")
+    return _page_arg(w, name, d, torch.float32)
+
+
+def _turned(x: Optional[torch.Tensor], out: Optional[torch.Tensor], name: str, like, n: int):
+    """Pointers, strides and heads of rows and of the rows they become."""
+    if x is None:
+        return None, 0, 0, None, 0
+    if out is None or x.shape != out.shape or x.dim() != 3:
+        raise ValueError(f"{name} and its output must both be [N, heads, d]")
+    if x.shape[0] != n:
+        raise ValueError(f"{name}: {n} rows are needed, got {x.shape[0]}")
+    H = x.shape[1]
+    xp, xs = _page_rows(x, name, H, like)
+    op, os_ = _page_rows(out, f"{name}_out", H, like)
+    return xp, xs, H, op, os_
+
+
+def prepare_norm_rotary(rotary, pos: torch.Tensor, q: Optional[torch.Tensor], q_out: Optional[torch.Tensor],
+                        k: Optional[torch.Tensor], k_out: Optional[torch.Tensor],
+                        q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                        eps: float = 1e-6, stream=None) -> Prepared:
+    """avtp_norm_rotary on fixed buffers, as a Prepared call (q or k may be None,
+    an output may be its input)."""
+    x = k if q is None else q
+    if x is None or x.dim() != 3:
+        raise ValueError("q or k [N, heads, d] is needed")
+    n, d, like = x.shape[0], x.shape[2], _Rows(x)
+    qp, qs, Hq, qo, qos = _turned(q, q_out, "q", like, n)
+    kp, ks, Hkv, ko, kos = _turned(k, k_out, "k", like, n)
+    pp, ps = _positions(rotary, pos, n)
+    args = (_stream(stream), rotary.ref(), dtype_code(x), d, n, pp, ps, _norm_weight(q_weight, "q_weight", d),
+            _norm_weight(k_weight, "k_weight", d), float(eps), qp, qs, Hq, qo, qos, kp, ks, Hkv, ko, kos)
+    return Prepared(lib().avtp_norm_rotary, args, "avtp_norm_rotary",
+                    (rotary, pos, q, q_out, k, k_out, q_weight, k_weight, stream))
+
+
+def norm_rotary(rotary, pos: torch.Tensor, q: Optional[torch.Tensor], k: Optional[torch.Tensor],
+                q_weight: Optional[torch.Tensor] = None, k_weight: Optional[torch.Tensor] = None,
+                eps: float = 1e-6, stream=None):
+    """Queries and keys [N, heads, d] normalised head by head (where a weight [d],
+    fp32, is given) and rotated by their positions (a ``Rotary``; pos [planes, N] or
+    [N] int64).  Returns (q_out, k_out)."""
+    new = lambda t: None if t is None else torch.empty(t.shape, dtype=t.dtype, device=t.device)  # noqa: E731
+    some = k if q is None else q
+    if some is None:
+        raise ValueError("q or k [N, heads, d] is needed")
+    with _on(stream, some.device):
+        q_out, k_out = new(q), new(k)
+    prepare_norm_rotary(rotary, pos, q, q_out, k, k_out, q_weight, k_weight, eps, stream)()
+    return q_out, k_out
+
+
+def prepare_page_store_rotary(pages: Pages, rotary, pos: torch.Tensor, q: Optional[torch.Tensor],
+                              q_out: Optional[torch.Tensor], k: torch.Tensor, v: torch.Tensor,
+                              slot_map: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                              k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                              stream=None) -> Prepared:
+    """avtp_page_store_rotary on fixed buffers, as a Prepared call: one row of q, k
+    and v for each entry of slot_map (q may be None)."""
+    n, d = slot_map.numel(), pages.d
+    kp, ks, vp, vs = page_store_rows(pages, k, v)
+    if k.shape[0] != n:
+        raise ValueError(f"slot_map has {n} entries, k and v {k.shape[0]} rows")
+    qp, qs, Hq, qo, qos = _turned(q, q_out, "q", pages, n)
+    pp, ps = _positions(rotary, pos, n)
+    args = (_stream(stream), pages.ref(), rotary.ref(), n, pp, ps, _norm_weight(q_weight, "q_weight", d),
+            _norm_weight(k_weight, "k_weight", d), float(eps), qp, qs, Hq, qo, qos, kp, ks, vp, vs,
+            _page_arg(slot_map, "slot_map"))
+    return Prepared(lib().avtp_page_store_rotary, args, "avtp_page_store_rotary",
+                    (pages, rotary, pos, q, q_out, k, v, slot_map, q_weight, k_weight, stream))
+
+
+def page_store_rotary(pages: Pages, rotary, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                      v: torch.Tensor, slot_map: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                      k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6, stream=None) -> torch.Tensor:
+    """``norm_rotary`` of a step's rows with K, and V as it is, on into their
+    slots of the pages.  Returns q_out."""
+    with _on(stream, q.device):
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    prepare_page_store_rotary(pages, rotary, pos, q, q_out, k, v, slot_map, q_weight, k_weight, eps, stream)()
+    return q_out

@@ -20,7 +20,8 @@ ARCH = "gfx950"
 
 SOURCES = ["avtp_api.cpp", "score_attn.hip", "finalize.hip", "score_variation.hip", "budget.hip",
            "select.hip", "compact.hip", "layer_stat.hip", "progressive.hip", "score_noalloc.hip",
-           "page_tables.hip", "page_store.hip", "page_attention.hip"]
+           "page_tables.hip", "page_store.hip", "page_attention.hip",
+           "page_share.hip", "rotary.hip"]
 
 FLAGS = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
          # packed fp32 ALU ops stay off on this target

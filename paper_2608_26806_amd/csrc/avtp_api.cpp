@@ -530,21 +530,177 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
                                       n_src, slot_map, keep_idx, n));
 }
 
-static int check_page_attention(const avtp_pages *pages, int Hq, int B, int64_t N_q, int64_t max_kv_len) {
+int avtp_page_fork(avtp_stream_t stream, int B, int page_size, const int32_t *parent,
+                   const int32_t *fork_len, const int32_t *seq_len, const int32_t *free_pages,
+                   int n_pages, const int32_t *free_count, int32_t *block_table, int max_pages,
+                   const int32_t *gone, int32_t *seq_len_out, int32_t *free_count_out,
+                   int32_t *src_page, int32_t *dst_page, int32_t *gone_out, int32_t *status) {
+  int rc = check_tables(B, page_size, max_pages, n_pages);
+  if (rc != AVTP_OK) return rc;
+  if (!parent || !fork_len || !seq_len || !free_pages || !free_count || !block_table || !seq_len_out ||
+      !free_count_out || !src_page || !dst_page || !gone != !gone_out)
+    return AVTP_ERR_INVALID_ARG;
+  // blocks read the state that another block would overwrite
+  for (const int32_t *out : {seq_len_out, src_page, dst_page, gone_out})
+    if (out && (out == parent || out == fork_len || out == seq_len || out == gone)) return AVTP_ERR_INVALID_ARG;
+  if (free_count_out == free_count) return AVTP_ERR_INVALID_ARG;
+  const PageFork F{B, __builtin_ctz((unsigned)page_size), max_pages, n_pages, parent, fork_len, seq_len, free_pages,
+                   free_count, gone, block_table, seq_len_out, free_count_out, src_page, dst_page, gone_out, status};
+  return hip_status(launch_page_fork((hipStream_t)stream, F));
+}
+
+int avtp_page_copy(avtp_stream_t stream, const avtp_pages *pages, const int32_t *src_page,
+                   const int32_t *dst_page, int64_t n) {
+  int rc = check_pages(pages);
+  if (rc != AVTP_OK) return rc;
+  if (n < 0) return AVTP_ERR_INVALID_ARG;
+  if (n > INT32_MAX) return AVTP_ERR_UNSUPPORTED;
+  if (n == 0) return AVTP_OK;
+  if (!src_page || !dst_page) return AVTP_ERR_INVALID_ARG;
+  return hip_status(launch_page_copy((hipStream_t)stream, *pages, src_page, dst_page, n));
+}
+
+size_t avtp_page_release_workspace_size(int n_pages) {
+  return n_pages < 1 ? 0 : page_release_workspace_bytes(n_pages);
+}
+
+int avtp_page_release(avtp_stream_t stream, int B, int page_size, const int32_t *keep_len,
+                      const int32_t *seq_len, const int32_t *block_table, int max_pages,
+                      int32_t *free_pages, int n_pages, const int32_t *free_count, int window,
+                      int sinks, const int32_t *gone, int32_t *seq_len_out,
+                      int32_t *free_count_out, int32_t *gone_out, int32_t *status, void *ws,
+                      size_t ws_bytes) {
+  int rc = check_tables(B, page_size, max_pages, n_pages);
+  if (rc != AVTP_OK) return rc;
+  if (!keep_len || !seq_len || !block_table || !free_pages || !free_count || !seq_len_out || !free_count_out ||
+      window < 0 || sinks < 0 || !gone != !gone_out || (window > 0 && !gone))
+    return AVTP_ERR_INVALID_ARG;
+  if (window > 1 << 30 || sinks > 1 << 30) return AVTP_ERR_UNSUPPORTED;
+  // (waves of one row read what another would overwrite)
+  for (const int32_t *out : {seq_len_out, gone_out})
+    if (out && (out == keep_len || out == seq_len || out == gone)) return AVTP_ERR_INVALID_ARG;
+  if (seq_len_out == gone_out || free_count_out == free_count) return AVTP_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < page_release_workspace_bytes(n_pages) || (uintptr_t)ws % 256) return AVTP_ERR_WORKSPACE;
+  const PageRelease R{B, __builtin_ctz((unsigned)page_size), max_pages, n_pages, window, sinks, keep_len, seq_len,
+                      block_table, free_count, gone, free_pages, seq_len_out, free_count_out, gone_out, status};
+  return hip_status(launch_page_release((hipStream_t)stream, R, (int32_t *)ws));
+}
+
+// a rotation, and what is common to its two calls (rows that are not there are not looked at)
+static int check_rotary(const avtp_rotary *rot, int d, int64_t n, const int64_t *pos, int64_t pos_stride, float eps) {
+  if (!rot || rot->rot_dim < 1 || rot->planes < 1 || n < 0 || !std::isfinite(rot->scale) || !std::isfinite(eps) ||
+      eps < 0.f)
+    return AVTP_ERR_INVALID_ARG;
+  if (rot->rot_dim % 16 || rot->rot_dim > d || rot->planes > AVTP_MAX_PLANES || n > INT32_MAX)
+    return AVTP_ERR_UNSUPPORTED;
+  if (!rot->turns || (uintptr_t)rot->turns % 8 || (uintptr_t)rot->plane % 4) return AVTP_ERR_INVALID_ARG;
+  if (n > 0 && (!pos || (uintptr_t)pos % 8)) return AVTP_ERR_INVALID_ARG;
+  if (rot->planes > 1 && (pos_stride < n || pos_stride > INT64_MAX / 64)) return AVTP_ERR_INVALID_ARG;
+  return AVTP_OK;
+}
+
+static bool in_place_ok(const void *x, int64_t stride, const void *out, int64_t out_stride) {
+  return x != out || stride == out_stride;
+}
+
+int avtp_norm_rotary(avtp_stream_t stream, const avtp_rotary *rotary, int dtype, int d, int64_t n,
+                     const int64_t *pos, int64_t pos_stride, const float *q_weight,
+                     const float *k_weight, float eps, const void *q, int64_t q_stride, int Hq,
+                     void *q_out, int64_t q_out_stride, const void *k, int64_t k_stride, int Hkv,
+                     void *k_out, int64_t k_out_stride) {
+  if (dtype != AVTP_BF16 && dtype != AVTP_FP32) return AVTP_ERR_UNSUPPORTED;
+  if (d != 64 && d != 128) return AVTP_ERR_UNSUPPORTED;
+  int rc = check_rotary(rotary, d, n, pos, pos_stride, eps);
+  if (rc != AVTP_OK) return rc;
+  if (Hq < 0 || Hkv < 0) return AVTP_ERR_INVALID_ARG;
+  if (Hq > 256 || Hkv > 256) return AVTP_ERR_UNSUPPORTED;
+  if (n == 0 || Hq + Hkv == 0) return AVTP_OK;
+  const avtp_pages rows{nullptr, nullptr, dtype, 0, 0, 0, d};
+  if (Hq > 0 && (!rows_ok(q, q_stride, Hq, rows) || !rows_ok(q_out, q_out_stride, Hq, rows) ||
+                 !in_place_ok(q, q_stride, q_out, q_out_stride)))
+    return AVTP_ERR_INVALID_ARG;
+  if (Hkv > 0 && (!rows_ok(k, k_stride, Hkv, rows) || !rows_ok(k_out, k_out_stride, Hkv, rows) ||
+                  !in_place_ok(k, k_stride, k_out, k_out_stride)))
+    return AVTP_ERR_INVALID_ARG;
+  const int64_t es = dtype == AVTP_FP32 ? 4 : 2;
+  RotaryArgs R{rotary->turns, rotary->plane, rotary->rot_dim, rotary->interleaved, rotary->planes, Hq, Hkv,
+               rotary->scale, eps, pos, pos_stride, q_weight, k_weight, (const char *)q, (const char *)k, nullptr,
+               (char *)q_out, (char *)k_out, nullptr, q_stride * es, q_out_stride * es, k_stride * es,
+               k_out_stride * es, 0, nullptr, n};
+  return hip_status(launch_norm_rotary((hipStream_t)stream, R, dtype, d, 0, 0));
+}
+
+int avtp_page_store_rotary(avtp_stream_t stream, const avtp_pages *pages, const avtp_rotary *rotary,
+                           int64_t n, const int64_t *pos, int64_t pos_stride,
+                           const float *q_weight, const float *k_weight, float eps, const void *q,
+                           int64_t q_stride, int Hq, void *q_out, int64_t q_out_stride,
+                           const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                           const int32_t *slot_map) {
+  int rc = check_pages(pages);
+  if (rc != AVTP_OK) return rc;
+  if ((rc = check_rotary(rotary, pages->d, n, pos, pos_stride, eps)) != AVTP_OK) return rc;
+  if (Hq < 0) return AVTP_ERR_INVALID_ARG;
+  if (Hq > 256) return AVTP_ERR_UNSUPPORTED;
+  if (n == 0) return AVTP_OK;
+  if (Hq > 0 && (!rows_ok(q, q_stride, Hq, *pages) || !rows_ok(q_out, q_out_stride, Hq, *pages) ||
+                 !in_place_ok(q, q_stride, q_out, q_out_stride)))
+    return AVTP_ERR_INVALID_ARG;
+  if (!slot_map || !rows_ok(k, k_stride, pages->Hkv, *pages) || !rows_ok(v, v_stride, pages->Hkv, *pages))
+    return AVTP_ERR_INVALID_ARG;
+  const int64_t es = pages->dtype == AVTP_FP32 ? 4 : 2;
+  RotaryArgs R{rotary->turns, rotary->plane, rotary->rot_dim, rotary->interleaved, rotary->planes, Hq, pages->Hkv,
+               rotary->scale, eps, pos, pos_stride, q_weight, k_weight, (const char *)q, (const char *)k,
+               (const char *)v, (char *)q_out, (char *)pages->k, (char *)pages->v, q_stride * es, q_out_stride * es,
+               k_stride * es, 0, v_stride * es, slot_map, n};
+  return hip_status(launch_norm_rotary((hipStream_t)stream, R, pages->dtype, pages->d, pages->page_size,
+                                       (int64_t)pages->n_pages * pages->page_size));
+}
+
+// window 0: every earlier token is seen
+static int check_page_attention(const avtp_pages *pages, int Hq, int B, int64_t N_q, int64_t max_kv_len,
+                                const PageWindow &w) {
   int rc = check_pages(pages);
   if (rc != AVTP_OK) return rc;
   if ((rc = check_attn_args(pages->dtype, Hq, pages->Hkv, pages->d)) != AVTP_OK) return rc;
   if (B < 1 || N_q < 0 || max_kv_len < 0) return AVTP_ERR_INVALID_ARG;
   if (B > AVTP_MAX_REQUESTS || N_q > INT32_MAX / Hq) return AVTP_ERR_UNSUPPORTED;
   // blocks of 256 threads, of which a launch has fewer than 2^32
-  if (page_attn_plan(*pages, Hq, B, N_q, max_kv_len).blocks >= 1 << 24) return AVTP_ERR_UNSUPPORTED;
+  if (page_attn_plan(*pages, Hq, B, N_q, max_kv_len, w).blocks >= 1 << 24) return AVTP_ERR_UNSUPPORTED;
   return AVTP_OK;
+}
+
+// a window that callers name, 0 if they must not
+static bool window_of(int window, int sinks, PageWindow *w) {
+  // no sequence has more than 2^30 tokens
+  *w = PageWindow{window < 1 << 30 ? window : 1 << 30, sinks < 1 << 30 ? sinks : 1 << 30};
+  return window >= 1 && sinks >= 0;
+}
+
+static int page_attention(avtp_stream_t stream, const avtp_pages *pages, const void *q,
+                          int64_t q_stride, int Hq, int B, int64_t N_q, const int32_t *cu_q,
+                          const int32_t *kv_len, const int32_t *block_table, int max_pages,
+                          int64_t max_kv_len, const PageWindow &w, float softmax_scale, void *out,
+                          int64_t out_stride, float *lse, int32_t *status, void *ws, size_t ws_bytes) {
+  int rc = check_page_attention(pages, Hq, B, N_q, max_kv_len, w);
+  if (rc != AVTP_OK) return rc;
+  if ((rc = check_tables(B, pages->page_size, max_pages, pages->n_pages)) != AVTP_OK) return rc;
+  if (!cu_q || !kv_len || !block_table || !std::isfinite(softmax_scale) || softmax_scale <= 0.f)
+    return AVTP_ERR_INVALID_ARG;
+  if (N_q > 0 && (!rows_ok(q, q_stride, Hq, *pages) || !rows_ok(out, out_stride, Hq, *pages)))
+    return AVTP_ERR_INVALID_ARG;
+  const PageAttnPlan L = page_attn_plan(*pages, Hq, B, N_q, max_kv_len, w);
+  if (L.bytes > 0 && (!ws || ws_bytes < L.bytes || (uintptr_t)ws % 256)) return AVTP_ERR_WORKSPACE;
+  if (N_q == 0) return AVTP_OK;
+  const int64_t es = pages->dtype == AVTP_FP32 ? 4 : 2;
+  const PageAttnArgs A{q,      out,    q_stride * es, out_stride * es, lse, cu_q,      kv_len,
+                       block_table, status, B,        Hq,              (int)N_q, max_pages, softmax_scale, w};
+  return hip_status(launch_page_attention((hipStream_t)stream, *pages, L, A, (char *)ws));
 }
 
 size_t avtp_page_attention_workspace_size(const avtp_pages *pages, int Hq, int B, int64_t N_q,
                                           int64_t max_kv_len) {
-  if (check_page_attention(pages, Hq, B, N_q, max_kv_len) != AVTP_OK) return 0;
-  return page_attn_plan(*pages, Hq, B, N_q, max_kv_len).bytes;
+  if (check_page_attention(pages, Hq, B, N_q, max_kv_len, PageWindow{}) != AVTP_OK) return 0;
+  return page_attn_plan(*pages, Hq, B, N_q, max_kv_len, PageWindow{}).bytes;
 }
 
 int avtp_page_attention(avtp_stream_t stream, const avtp_pages *pages, const void *q,
@@ -552,20 +708,28 @@ int avtp_page_attention(avtp_stream_t stream, const avtp_pages *pages, const voi
                         const int32_t *kv_len, const int32_t *block_table, int max_pages,
                         int64_t max_kv_len, float softmax_scale, void *out, int64_t out_stride,
                         float *lse, int32_t *status, void *ws, size_t ws_bytes) {
-  int rc = check_page_attention(pages, Hq, B, N_q, max_kv_len);
-  if (rc != AVTP_OK) return rc;
-  if ((rc = check_tables(B, pages->page_size, max_pages, pages->n_pages)) != AVTP_OK) return rc;
-  if (!cu_q || !kv_len || !block_table || !std::isfinite(softmax_scale) || softmax_scale <= 0.f)
-    return AVTP_ERR_INVALID_ARG;
-  if (N_q > 0 && (!rows_ok(q, q_stride, Hq, *pages) || !rows_ok(out, out_stride, Hq, *pages)))
-    return AVTP_ERR_INVALID_ARG;
-  const PageAttnPlan L = page_attn_plan(*pages, Hq, B, N_q, max_kv_len);
-  if (L.bytes > 0 && (!ws || ws_bytes < L.bytes || (uintptr_t)ws % 256)) return AVTP_ERR_WORKSPACE;
-  if (N_q == 0) return AVTP_OK;
-  const int64_t es = pages->dtype == AVTP_FP32 ? 4 : 2;
-  const PageAttnArgs A{q,      out,    q_stride * es, out_stride * es, lse, cu_q,      kv_len,
-                       block_table, status, B,        Hq,              (int)N_q, max_pages, softmax_scale};
-  return hip_status(launch_page_attention((hipStream_t)stream, *pages, L, A, (char *)ws));
+  return page_attention(stream, pages, q, q_stride, Hq, B, N_q, cu_q, kv_len, block_table, max_pages, max_kv_len,
+                        PageWindow{}, softmax_scale, out, out_stride, lse, status, ws, ws_bytes);
+}
+
+size_t avtp_page_attention_window_workspace_size(const avtp_pages *pages, int Hq, int B,
+                                                 int64_t N_q, int64_t max_kv_len, int window,
+                                                 int sinks) {
+  PageWindow w;
+  if (!window_of(window, sinks, &w) || check_page_attention(pages, Hq, B, N_q, max_kv_len, w) != AVTP_OK) return 0;
+  return page_attn_plan(*pages, Hq, B, N_q, max_kv_len, w).bytes;
+}
+
+int avtp_page_attention_window(avtp_stream_t stream, const avtp_pages *pages, const void *q,
+                               int64_t q_stride, int Hq, int B, int64_t N_q, const int32_t *cu_q,
+                               const int32_t *kv_len, const int32_t *block_table, int max_pages,
+                               int64_t max_kv_len, int window, int sinks, float softmax_scale,
+                               void *out, int64_t out_stride, float *lse, int32_t *status,
+                               void *ws, size_t ws_bytes) {
+  PageWindow w;
+  if (!window_of(window, sinks, &w)) return AVTP_ERR_INVALID_ARG;
+  return page_attention(stream, pages, q, q_stride, Hq, B, N_q, cu_q, kv_len, block_table, max_pages, max_kv_len, w,
+                        softmax_scale, out, out_stride, lse, status, ws, ws_bytes);
 }
 
 }  // extern "C"

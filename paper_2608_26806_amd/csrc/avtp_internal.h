@@ -140,6 +140,42 @@ hipError_t launch_page_store(hipStream_t stream, const avtp_pages &P, const void
                              int64_t n_src, const int32_t *slot_map, const int32_t *keep_idx,
                              int64_t n);
 
+// Pages named by several sequences: new sequences that start from others'
+// tokens, whole pages copied, pages handed back that no sequence names any more.
+struct PageFork {
+  int B, page_shift, max_pages, n_pages;
+  const int32_t *parent, *fork_len, *seq_len, *free_pages, *free_count, *gone;
+  int32_t *table, *seq_len_out, *free_count_out, *src_page, *dst_page, *gone_out, *status;
+};
+hipError_t launch_page_fork(hipStream_t stream, const PageFork &F);
+hipError_t launch_page_copy(hipStream_t stream, const avtp_pages &P, const int32_t *src_page,
+                            const int32_t *dst_page, int64_t n);
+struct PageRelease {
+  int B, page_shift, max_pages, n_pages, window, sinks;
+  const int32_t *keep_len, *seq_len, *table, *free_count, *gone;
+  int32_t *free_pages, *seq_len_out, *free_count_out, *gone_out, *status;
+};
+size_t page_release_workspace_bytes(int n_pages);
+hipError_t launch_page_release(hipStream_t stream, const PageRelease &R, int32_t *ws);
+
+// Norm and rotation of rows, into rows or (slot: K and V) into pages.
+struct RotaryArgs {
+  const uint64_t *turns;
+  const int32_t *plane;
+  int rot, interleaved, planes, Hq, Hk;
+  float scale, eps;
+  const int64_t *pos;
+  int64_t pos_stride;  // positions from one plane to the next
+  const float *q_weight, *k_weight;
+  const char *q, *k, *v;
+  char *q_out, *k_out, *v_out;
+  int64_t q_tok, q_out_tok, k_tok, k_out_tok, v_tok;  // bytes from one token to the next
+  const int32_t *slot;
+  int64_t n;
+};
+hipError_t launch_norm_rotary(hipStream_t stream, const RotaryArgs &R, int dtype, int d,
+                              int page_size, int64_t slots);
+
 // Attention over the pages: its launch, from host-known sizes only (so the
 // workspace size and the launch always agree).
 struct PageAttnPlan {
@@ -153,7 +189,13 @@ struct PageAttnPlan {
   int cuts;        // tiles that may have been cut, and how many parts they may leave:
   size_t off_lse, off_meta, bytes;  // rows fp32, their log2 sums, whose they are
 };
-PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len);
+// A row at position p sees the tokens up to it that lie behind p - window or before
+// `sinks`; window 0: all of them.
+struct PageWindow {
+  int window, sinks;
+};
+PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len,
+                            const PageWindow &w);
 
 struct PageAttnArgs {
   const void *q;
@@ -164,6 +206,7 @@ struct PageAttnArgs {
   int32_t *status;
   int B, Hq, N_q, max_pages;
   float scale;
+  PageWindow w;
 };
 hipError_t launch_page_attention(hipStream_t stream, const avtp_pages &P, const PageAttnPlan &L,
                                  const PageAttnArgs &A, char *ws);

@@ -84,6 +84,7 @@ __device__ inline void put4(char *row, int dd, f32x4 x) {
 }
 
 struct KArgs {
+  static constexpr bool WIN = false;
   const char *q, *k, *v;
   char *out;
   long long q_tok, out_tok, head_bytes;  // head_bytes: one head of one page
@@ -95,6 +96,11 @@ struct KArgs {
   float gain, from;
   int4 *meta;                  // two per possible cut tile
   float cl2e;
+};
+// Rows that see a window of the latest tokens and the first ones (PageWindow).
+struct WArgs : KArgs {
+  static constexpr bool WIN = true;
+  int window, sinks;
 };
 
 // A buffer of `bytes` bytes at p, both the same in every lane (said once more
@@ -182,14 +188,32 @@ template <int BM>
 __device__ inline int tiles_of(const KArgs &a, const Seq &s) {
   return (s.n * a.G + BM - 1) / BM;
 }
-// keys that the last row of a tile sees
-template <int BM>
-__device__ inline int tile_keys(const KArgs &a, const Seq &s, int tile) {
-  return min(s.L, s.kv - s.n + (min((tile + 1) * BM, s.n * a.G) - 1) / a.G + 1);
+// The keys of a tile, of which its rows see some: with a window, the stages that hold
+// the sinks and then, from the 16 keys on in which the first row's window starts, those
+// up to the last row.  They are numbered without what lies between, so that all work is
+// shared out by number: number x is key x up to `head`, then key x + skip.
+struct Span {
+  int keys;                // their number
+  int head, skip, lo;      // lo: the first key behind the sinks that a row sees
+  __device__ inline int key(int x) const { return x < head ? x : x + skip; }
+};
+template <int BM, int KS, typename A>
+__device__ inline Span span_of(const A &a, const Seq &s, int tile) {
+  const int hi = min(s.L, s.kv - s.n + (min((tile + 1) * BM, s.n * a.G) - 1) / a.G + 1);
+  if constexpr (A::WIN) {
+    const int lo = max(0, s.kv - s.n + tile * BM / a.G + 1 - a.window);
+    const int head = (a.sinks + KS - 1) / KS * KS;
+    // (a table that ends before the window)
+    if (lo >= hi) return {min(hi, a.sinks), head, 0, lo};
+    const int skip = max(0, (lo & ~15) - head);
+    return {hi - skip, head, skip, lo};
+  } else {
+    return {hi, 0, 0, 0};
+  }
 }
-template <int BM, int KS>
-__device__ inline int units_of(const KArgs &a, const Seq &s, int tile) {
-  return max(1, (tile_keys<BM>(a, s, tile) + KS - 1) / KS);
+template <int BM, int KS, typename A>
+__device__ inline int units_of(const A &a, const Seq &s, int tile) {
+  return max(1, (span_of<BM, KS>(a, s, tile).keys + KS - 1) / KS);
 }
 typedef uint64_t u64;
 // inclusive, over the lanes; v below 2^50
@@ -197,8 +221,8 @@ __device__ inline u64 prefix_sum64(u64 v) {
   return (u64)wave::prefix_sum((uint32_t)(v & 0xFFFFFF)) + ((u64)wave::prefix_sum((uint32_t)(v >> 24)) << 24);
 }
 // Units of lane i's sequence c0 + i (0 behind the last); every lane calls it.
-template <int BM, int KS>
-__device__ inline u64 seq_units(const KArgs &a, int c0, Seq &s) {
+template <int BM, int KS, typename A>
+__device__ inline u64 seq_units(const A &a, int c0, Seq &s) {
   const int lane = threadIdx.x & 63, b = c0 + lane;
   s = seq_of(a, min(b, a.B - 1));
   const int T = b < a.B ? tiles_of<BM>(a, s) : 0;
@@ -224,7 +248,8 @@ struct Place {
   Seq s;
   // the place of unit w of the `per` units of a key head (first: the first 64
   // sequences' units and descriptions)
-  __device__ inline void find(const KArgs &a, u64 w, u64 per, u64 units, const Seq &first) {
+  template <typename A>
+  __device__ inline void find(const A &a, u64 w, u64 per, u64 units, const Seq &first) {
     const int lane = threadIdx.x & 63;
     g = (int)(w / per);
     u64 r = w - (u64)g * per;
@@ -258,7 +283,8 @@ struct Place {
     }
   }
   // the first unit of the next tile (there is one)
-  __device__ inline void next(const KArgs &a) {
+  template <typename A>
+  __device__ inline void next(const A &a) {
     u = 0;
     if (++t >= tiles_of<BM>(a, s)) {
       t = 0;
@@ -299,7 +325,7 @@ __device__ inline Cut get_cut(const int4 *meta, int i) {
 }
 
 // One tile (or, cut, some of its keys): the rows row0 .. of sequence b and key
-// head g over keys kbeg .. kend - 1.
+// head g over the keys of number kbeg .. kend - 1 (kbeg: the first of a stage).
 struct Job {
   int g, b, row0, kbeg, kend, slot;  // slot: where a cut tile's part goes
   bool cut;
@@ -327,8 +353,8 @@ struct Shape {
 };
 
 // HERE: the part stays in LDS, rows of D floats in bufA and their log2 sums in sums.
-template <typename T, int D, int M, int WR, int TPW, bool HERE = false>
-__device__ __attribute__((always_inline)) inline void attend(const KArgs &a, const Job &job, AVTP_LDS char *bufA,
+template <typename T, int D, int M, int WR, int TPW, bool HERE = false, typename A>
+__device__ __attribute__((always_inline)) inline void attend(const A &a, const Job &job, AVTP_LDS char *bufA,
                                                              AVTP_LDS char *bufB, AVTP_LDS float *sums = nullptr) {
   using G_ = Geo<T, D>;
   using S_ = Shape<T, D, M, WR, TPW>;
@@ -357,6 +383,24 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   const int lim = min(L, job.s.kv - job.s.n + tok + 1);
   const bool valid = wrow + col < R;
   const int wmin = __builtin_amdgcn_readlane(lim, 0), wmax = __builtin_amdgcn_readlane(lim, M - 1);
+  // the row's window starts at key `low`, of the wave's rows at wlow .. wlow1
+  constexpr bool WIN = A::WIN;
+  const Span span = span_of<BM, KS>(a, job.s, row0 / BM);
+  int sinks = 0, low = 0, wlow = 0, wlow1 = 0;
+  if constexpr (WIN) {
+    sinks = a.sinks;
+    low = job.s.kv - job.s.n + tok + 1 - a.window;
+    wlow = __builtin_amdgcn_readlane(low, 0);
+    wlow1 = __builtin_amdgcn_readlane(low, M - 1);
+  }
+  auto sees = [&](int key) __attribute__((always_inline)) {
+    return WIN ? key < lim && (key < sinks || key >= low) : key < lim;
+  };
+  // do all rows of the wave see the n keys from number x, which is key `key`, on?
+  auto all_see = [&](int x, int key, int n) __attribute__((always_inline)) {
+    if (WIN) return x + n <= kend && key + n <= wmin && (key + n <= sinks || key >= wlow1);
+    return x + n <= min(kend, wmin);
+  };
 
   // where this lane's loads of a 16-row group come from
   uint32_t voff[LPG];
@@ -376,9 +420,10 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   }
 
   const int32_t *trow = a.table + (long long)b * a.max_pages;
-  // page ids of the wave's groups of the stage at key ks, one per lane (lane
+  // page ids of the wave's groups of the stage at number x, one per lane (lane
   // gi: group gi), read a stage ahead
-  auto load_ids = [&](int ks) __attribute__((always_inline)) {
+  auto load_ids = [&](int x) __attribute__((always_inline)) {
+    const int ks = WIN ? span.key(x) : x;
     const int key = min(ks + r0w + (lane & (NG - 1)) * 16, L - 1);
     return trow[key >> a.page_shift];
   };
@@ -386,13 +431,16 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
   // Chunks, 32-row tiles of the short form among them, read them again, from the L2
   // (eight of 30 tokens over 1,500 keys, 32/8 heads, 23.1 us non-temporal, 20.9 so).
   constexpr int kAux = WR == 1 && !(HERE && M == 32) ? 2 : 0;
-  auto issue = [&](AVTP_LDS char *buf, int ks, int ids) __attribute__((always_inline)) {
+  auto issue = [&](AVTP_LDS char *buf, int x, int ids) __attribute__((always_inline)) {
+    const int ks = WIN ? span.key(x) : x;
 #pragma unroll
     for (int gi = 0; gi < NG; ++gi) {
       const int id = __builtin_amdgcn_readlane(ids, gi);
       const int key = ks + r0w + gi * 16;
-      const bool ok = (unsigned)id < (unsigned)a.n_pages;
-      if (!ok && key < L && a.status && lane == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
+      // (between the sinks and the window a page need not be there)
+      const bool seen = !WIN || key < sinks || key + GR > span.lo;
+      const bool ok = seen && (unsigned)id < (unsigned)a.n_pages;
+      if (!ok && seen && key < L && a.status && lane == 0) atomicOr(&a.status[b], AVTP_FLAG_BAD_PAGE);
       const int have = ok ? min(max(L - key, 0), GR) * ROWB : 0;
       const long long off = ok ? ((long long)id * a.Hkv + g) * a.head_bytes + (long long)(key & pmask) * ROWB : 0;
       const Rsrc rk = make_rsrc(a.k + off, have), rv = make_rsrc(a.v + off, have);
@@ -465,10 +513,10 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     }
     return __ballot(bad) != 0ull;
   };
-  auto add_not_finite = [&](lptr vt, int kb) __attribute__((always_inline)) {
+  auto add_not_finite = [&](lptr vt, int key) __attribute__((always_inline)) {
 #pragma unroll 1
     for (int r = 0; r < kTile; ++r) {
-      const bool seen = kb + r < lim;
+      const bool seen = sees(key + r);
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
 #pragma unroll
@@ -634,16 +682,17 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     }
     return TPW;
   };
-  // A tile of keys from kb on, of which some rows may see a part or nothing, and
+  // A tile of keys from number kb on, of which some rows may see a part or nothing, and
   // whose largest logit becomes the row's reference if it is larger.
   auto part = [&](lptr kt, lptr vt, int kb) __attribute__((always_inline)) {
+    const int key = WIN ? span.key(kb) : kb;
     Logits S = logits(kt);
     Probs p;
     float top = -INFINITY;
 #pragma unroll
     for (int e = 0; e < NE; ++e) {
       float &x = reinterpret_cast<float *>(&S)[e];
-      x = kb + 4 * grp + eoff(e) < lim ? x : -INFINITY;
+      x = sees(key + 4 * grp + eoff(e)) ? x : -INFINITY;
       top = fmaxf(top, x);
     }
     const float nm = fmaxf(m, over_row<M>(top, [](float x, float y) { return fmaxf(x, y); }) * cl2e);
@@ -657,8 +706,8 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
         for (int e = 0; e < AE; ++e) O[dt][e] *= f;
     }
     l += probs(S, p, m == -INFINITY ? 0.f : m);  // (no key seen so far: every term is 0)
-    if (kb + kTile > min(kend, wmin) && __builtin_expect(tile_not_finite(vt), 0)) {
-      add_not_finite(vt, kb);
+    if (!all_see(kb, key, kTile) && __builtin_expect(tile_not_finite(vt), 0)) {
+      add_not_finite(vt, key);
       weigh(vt, p, true);
     } else {
       weigh(vt, p, false);
@@ -685,15 +734,21 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
     // every read would wait for the loads)
     auto parts = [&](AVTP_LDS const char *__restrict__ cur, int st, int from) __attribute__((always_inline)) {
       // keys below the range's end, and those that rows of this wave see
-      const int ks = kbeg + st * KS, stop = min(kend, wmax);
+      const int ks = kbeg + st * KS, stop = min(kend, wmax), key = WIN ? span.key(ks) : ks;
+      auto some_see = [&](int t) __attribute__((always_inline)) {
+        if (!WIN) return ks + t * kTile < stop;
+        const int x = key + t * kTile;
+        return ks + t * kTile < kend && x < wmax && (x < sinks || x + kTile > wlow);
+      };
 #pragma unroll 1
       for (int t = from; t < TPW; ++t)
-        if (ks + t * kTile < stop) part(cur + t * kTile * ROWB, cur + TB + t * kTile * ROWB, ks + t * kTile);
+        if (some_see(t)) part(cur + t * kTile * ROWB, cur + TB + t * kTile * ROWB, ks + t * kTile);
     };
     auto wholes = [&](AVTP_LDS const char *__restrict__ cur, AVTP_LDS char *__restrict__ nxt, int st)
         __attribute__((always_inline)) {
       begin(nxt, st);
-      return __builtin_expect(kbeg + (st + 1) * KS <= min(kend, wmin), 1) ? whole(cur, cur + TB) : 0;
+      const int ks = kbeg + st * KS;
+      return __builtin_expect(all_see(ks, WIN ? span.key(ks) : ks, KS), 1) ? whole(cur, cur + TB) : 0;
     };
     // Stages whose keys every row sees run in a loop of their own (with both
     // kinds in one, O was copied at every stage); the first one, and those that
@@ -739,8 +794,8 @@ __device__ __attribute__((always_inline)) inline void attend(const KArgs &a, con
 
 // Few rows per sequence (decode steps): a block is one wave, a worker that takes
 // its share of the line of units.
-template <typename T, int D, int M>
-__global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_attn_few_kernel(KArgs a) {
+template <typename T, int D, int M, typename A>
+__global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_attn_few_kernel(A a) {
   using S_ = Shape<T, D, M, 1, 1>;
   constexpr int BM = S_::BM, KS = S_::KS;
   // two stage buffers as distinct objects, so the compiler can tell the one
@@ -766,7 +821,7 @@ __global__ __launch_bounds__(64, (Shape<T, D, M, 1, 1>::kPerSimd)) void page_att
     at.find(a, w, per, units, first);
     for (;;) {
       const int u1 = (u64)(at.U - at.u) <= wend - w ? at.U : at.u + (int)(wend - w);
-      Job job{at.g, at.b, at.t * BM, at.u * KS, min(tile_keys<BM>(a, at.s, at.t), u1 * KS),
+      Job job{at.g, at.b, at.t * BM, at.u * KS, min(span_of<BM, KS>(a, at.s, at.t).keys, u1 * KS),
               2 * worker + (at.u > 0 ? 0 : 1), at.u > 0 || u1 < at.U, at.s};
       attend<T, D, M, 1, 1>(a, job, (AVTP_LDS char *)smA, (AVTP_LDS char *)smB);
       // (a worker's first part of a tile is the odd one of its slots; the
@@ -821,8 +876,8 @@ __device__ inline int tile_of_rank(const KArgs &a, int rank, int &b, Seq &s) {
 // Short work: a block takes a whole tile, its W waves a share of the
 // keys each, and joins their parts in LDS: no second launch.
 constexpr int kShortWaves = 4;  // whose buffers a CU's LDS holds
-template <typename T, int D, int M>
-__global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(KArgs a) {
+template <typename T, int D, int M, typename A>
+__global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(A a) {
   using S_ = Shape<T, D, M, 1, 1>;
   constexpr int KS = S_::KS, BUF = 2 * S_::TB, W = kShortWaves;
   static_assert(M * D * 4 <= BUF, "a part fits a stage buffer");
@@ -835,7 +890,7 @@ __global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(KArgs
   Seq s{};
   const int tile = tile_of_rank<M>(a, blockIdx.x / a.Hkv, b, s);
   if (tile < 0) return;
-  const int keys = tile_keys<M>(a, s, tile), units = units_of<M, KS>(a, s, tile), each = (units + W - 1) / W;
+  const int keys = span_of<M, KS>(a, s, tile).keys, units = units_of<M, KS>(a, s, tile), each = (units + W - 1) / W;
   const Job job{g, b, tile * M, wave * each * KS, min(keys, (wave + 1) * each * KS), 0, true, s};
   attend<T, D, M, 1, 1, true>(a, job, (AVTP_LDS char *)smA + wave * BUF, (AVTP_LDS char *)smB + wave * BUF,
                               (AVTP_LDS float *)sums + wave * M);
@@ -888,8 +943,8 @@ __host__ __device__ inline int key_ranges(int keys, float gain, float from) {
 // an XCD (blocks equal mod 8) reads the same K and V at about the same time: in
 // the even line above, whose workers stand at different keys, four prompts of
 // 7,000-9,000 tokens took 2907 us, with blocks in step 2147.
-template <typename T, int D, int WR, int TPW>
-__global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void page_attn_many_kernel(KArgs a) {
+template <typename T, int D, int WR, int TPW, typename A>
+__global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void page_attn_many_kernel(A a) {
   using S_ = Shape<T, D, 32, WR, TPW>;
   constexpr int BM = S_::BM, KS = S_::KS;
   __shared__ __attribute__((aligned(16))) char smA[2 * S_::TB];
@@ -902,7 +957,7 @@ __global__ __launch_bounds__(64 * WR, (Shape<T, D, 32, WR, TPW>::kPerSimd)) void
   const int tile = tile_of_rank<BM>(a, rank, b, s);
   Cut c{};
   if (tile >= 0) {
-    const int keys = tile_keys<BM>(a, s, tile);
+    const int keys = span_of<BM, KS>(a, s, tile).keys;
     // whole stages, evenly
     const int stages = max(1, (keys + KS - 1) / KS);
     const int ranges = min(a.nsplit, max(1, key_ranges<KS>(keys, a.gain, a.from)));
@@ -1019,10 +1074,13 @@ constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
 }  // namespace
 
-PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len) {
+PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int64_t max_kv_len,
+                            const PageWindow &w) {
   PageAttnPlan L{};
   // (longer sequences run all the same)
   max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
+  // what a row sees (a tile's first rows see a few more keys than its last)
+  if (w.window > 0 && max_kv_len > (int64_t)w.window + w.sinks) max_kv_len = (int64_t)w.window + w.sinks;
   const int64_t rows = N_q * (Hq / P.Hkv);
   // one wave of 16 or 32 rows for a sequence, or blocks of 128; a tile's ranks: at most
   auto tiles_of = [&](int bm) { return (rows / bm + B) * P.Hkv; };
@@ -1095,26 +1153,27 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   return L;
 }
 
-template <typename T, int D>
-static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) {
+template <typename T, int D, typename A>
+static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const A &k) {
   constexpr int TPW = many_tiles(D * (int)sizeof(T));
   const dim3 grid((unsigned)L.blocks);
   if constexpr (sizeof(T) == 2) {
     if (L.brief) {
-      if (L.tile == 16) hipLaunchKernelGGL((page_attn_short_kernel<T, D, 16>), grid, dim3(64 * kShortWaves), 0, st, k);
-      else hipLaunchKernelGGL((page_attn_short_kernel<T, D, 32>), grid, dim3(64 * kShortWaves), 0, st, k);
+      if (L.tile == 16) hipLaunchKernelGGL((page_attn_short_kernel<T, D, 16, A>), grid, dim3(64 * kShortWaves), 0, st, k);
+      else hipLaunchKernelGGL((page_attn_short_kernel<T, D, 32, A>), grid, dim3(64 * kShortWaves), 0, st, k);
       return hipGetLastError();
     }
   }
-  if (L.tile == 16) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 16>), grid, dim3(64), 0, st, k);
-  else if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 32>), grid, dim3(64), 0, st, k);
-  else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW>), grid, dim3(64 * kManyWaves), 0, st, k);
+  if (L.tile == 16) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 16, A>), grid, dim3(64), 0, st, k);
+  else if (L.few) hipLaunchKernelGGL((page_attn_few_kernel<T, D, 32, A>), grid, dim3(64), 0, st, k);
+  else hipLaunchKernelGGL((page_attn_many_kernel<T, D, kManyWaves, TPW, A>), grid, dim3(64 * kManyWaves), 0, st, k);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || L.cuts == 0) return e;
   // (a block per 2048 / D rows, one for a shorter tile)
   auto join = [&](auto bm_tag) {
     constexpr int BM = decltype(bm_tag)::value, ROWS = kJoinThreads * 4 / D < BM ? kJoinThreads * 4 / D : BM;
-    hipLaunchKernelGGL((page_join_kernel<T, D, BM>), dim3((unsigned)(L.cuts * (BM / ROWS))), dim3(ROWS * D / 4), 0, st, k);
+    hipLaunchKernelGGL((page_join_kernel<T, D, BM>), dim3((unsigned)(L.cuts * (BM / ROWS))), dim3(ROWS * D / 4), 0, st,
+                       (const KArgs &)k);
   };
   if (L.tile == 16) join(std::integral_constant<int, 16>{});
   else if (L.few) join(std::integral_constant<int, 32>{});
@@ -1122,10 +1181,18 @@ static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const KArgs &k) 
   return hipGetLastError();
 }
 
+template <typename A>
+static hipError_t launch(hipStream_t st, const avtp_pages &P, const PageAttnPlan &L, const A &k) {
+  if (P.dtype == AVTP_FP32) return P.d == 64 ? launch<float, 64>(st, L, k) : launch<float, 128>(st, L, k);
+  return P.d == 64 ? launch<__bf16, 64>(st, L, k) : launch<__bf16, 128>(st, L, k);
+}
+
 hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const PageAttnPlan &L,
                                  const PageAttnArgs &A, char *ws) {
   clear_pending_error();
-  KArgs k;
+  WArgs k;
+  k.window = A.w.window;
+  k.sinks = A.w.sinks;
   k.q = (const char *)A.q;
   k.k = (const char *)P.k;
   k.v = (const char *)P.v;
@@ -1154,8 +1221,7 @@ hipError_t launch_page_attention(hipStream_t st, const avtp_pages &P, const Page
   k.gain = L.gain;
   k.from = L.from;
   k.cl2e = A.scale * kLog2e;
-  if (P.dtype == AVTP_FP32) return P.d == 64 ? launch<float, 64>(st, L, k) : launch<float, 128>(st, L, k);
-  return P.d == 64 ? launch<__bf16, 64>(st, L, k) : launch<__bf16, 128>(st, L, k);
+  return A.w.window > 0 ? launch(st, P, L, k) : launch(st, P, L, (const KArgs &)k);
 }
 
 }  // namespace avtp

@@ -1,0 +1,342 @@
+// Pages that several sequences name: new sequences that start from another's
+// tokens, copies of whole pages, and pages handed back when no row of the table
+// names them any more.
+//
+// No counts of a page's holders are kept between calls, where they could go out
+// of step with the table: a release counts them from the rows, which it has to
+// read in part anyway (64 sequences of 500 pages: 128 KB).  Forks and releases are
+// bound by latency, copies by the memory's rate.
+#include <hip/hip_runtime.h>
+
+#include <stdint.h>
+
+#include "avtp_internal.h"
+#include "wave_ops.h"
+
+namespace avtp {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
+
+__device__ inline int pages_of(int tokens, int shift) { return (int)(((long long)tokens + (1 << shift) - 1) >> shift); }
+__device__ inline bool in_pool(int id, int n_pages) { return (unsigned)id < (unsigned)n_pages; }
+
+// the sum over the block's threads (every thread gets it)
+template <int WAVES>
+__device__ inline int block_sum(int v, int *wsum) {
+  const int s = (int)wave::sum((uint32_t)v);
+  __syncthreads();  // wsum's last readers are done
+  if ((threadIdx.x & 63) == 0) wsum[threadIdx.x >> 6] = s;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) total += wsum[w];
+  return total;
+}
+
+// ---- forks
+
+struct Fork {
+  int parent, len;  // parent < 0: the sequence stays as it was
+  int need;         // 1: its last page is partly filled, it gets one of its own
+  bool refused;
+};
+__device__ inline Fork fork_of(const PageFork &a, int b) {
+  Fork f{a.parent[b], 0, 0, false};
+  if (f.parent < 0) return f;
+  f.len = a.fork_len[b];
+  bool ok = f.parent < a.B && a.seq_len[b] <= 0;
+  if (ok) {
+    const int L = max(0, a.seq_len[f.parent]);
+    ok = a.parent[f.parent] < 0 && f.len >= 0 && f.len <= L && pages_of(f.len, a.page_shift) <= a.max_pages &&
+         (!a.gone || a.gone[f.parent] <= 0 || f.len == L);
+  }
+  if (!ok) return Fork{-1, 0, 0, true};
+  f.need = (f.len & ((1 << a.page_shift) - 1)) != 0;
+  return f;
+}
+
+// Block i makes the forks of its per_block sequences (a wave each at a time),
+// after counting the pages that the sequences before them take.  Rows that are
+// read are not written: a parent is no fork of the same call.
+struct FArgs {
+  PageFork f;
+  int per_block;
+};
+__global__ __launch_bounds__(kThreads) void page_fork_kernel(FArgs x) {
+  __shared__ int wsum[kWaves];
+  const PageFork &a = x.f;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int count = min(max(0, a.free_count[0]), a.n_pages);
+  const int b0 = blockIdx.x * x.per_block, b1 = min(b0 + x.per_block, a.B);
+  int sum = 0;
+  for (int b = tid; b < b0; b += kThreads) sum += fork_of(a, b).need;
+  const int before = block_sum<kWaves>(sum, wsum);
+  // lane j: the block's sequence j (every wave holds them all)
+  const int b = b0 + lane;
+  Fork f{-1, 0, 0, false};
+  if (b < b1) f = fork_of(a, b);
+  const int end = before + (int)wave::prefix_sum((uint32_t)f.need);
+  const bool fits = f.need == 0 || end <= count;
+  int src = -1, dst = -1;
+  if (f.parent >= 0 && f.need && fits) {
+    src = a.table[(size_t)f.parent * a.max_pages + (f.len >> a.page_shift)];
+    dst = a.free_pages[count - end];
+  }
+  for (int j = wave; j < b1 - b0; j += kWaves) {
+    const int parent = __builtin_amdgcn_readlane(f.parent, j), len = __builtin_amdgcn_readlane(f.len, j);
+    if (parent < 0 || !__builtin_amdgcn_readlane((int)fits, j)) continue;
+    const int whole = len >> a.page_shift, fresh = __builtin_amdgcn_readlane(dst, j);
+    const int32_t *from = a.table + (size_t)parent * a.max_pages;
+    int32_t *to = a.table + (size_t)(b0 + j) * a.max_pages;
+    for (int i = lane; i < whole; i += 64) to[i] = from[i];
+    if (lane == 0 && __builtin_amdgcn_readlane(f.need, j)) to[whole] = fresh;
+  }
+  if (wave == 0 && b < b1) {
+    const bool made = f.parent >= 0 && fits;
+    const bool good = in_pool(src, a.n_pages) && in_pool(dst, a.n_pages);
+    a.seq_len_out[b] = made ? f.len : a.seq_len[b];
+    a.src_page[b] = good ? src : -1;
+    a.dst_page[b] = good ? dst : -1;
+    if (a.gone) a.gone_out[b] = made ? a.gone[f.parent] : a.gone[b];
+    const int flags = (f.refused ? AVTP_FLAG_REFUSED : 0) | (fits ? 0 : AVTP_FLAG_NO_PAGES) |
+                      (made && f.need && !good ? AVTP_FLAG_BAD_PAGE : 0);
+    if (flags && a.status) atomicOr(&a.status[b], flags);
+  }
+  if (b1 == a.B && tid == 63) a.free_count_out[0] = count - min(end, count);
+}
+
+// ---- copies of pages
+
+struct CArgs {
+  char *k, *v;
+  const int32_t *src, *dst;
+  long long page_bytes;
+  int chunks, n_pages;  // chunks of a page, blocks of one page and tensor
+};
+constexpr int kUnits = 4;  // of 16 bytes, per thread
+__global__ __launch_bounds__(kThreads) void page_copy_kernel(CArgs a) {
+  const unsigned i = blockIdx.x / (2 * a.chunks), part = blockIdx.x % (2 * a.chunks);
+  const int src = a.src[i], dst = a.dst[i];
+  if (!in_pool(src, a.n_pages) || !in_pool(dst, a.n_pages)) return;
+  char *base = part & 1 ? a.v : a.k;
+  const uint4 *from = reinterpret_cast<const uint4 *>(base + src * a.page_bytes);
+  uint4 *to = reinterpret_cast<uint4 *>(base + dst * a.page_bytes);
+  const int units = (int)(a.page_bytes / 16), u0 = (int)(part >> 1) * kThreads * kUnits + threadIdx.x;
+  uint4 x[kUnits];
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u)
+    if (u0 + u * kThreads < units) x[u] = from[u0 + u * kThreads];
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u)
+    if (u0 + u * kThreads < units) to[u0 + u * kThreads] = x[u];
+}
+
+// ---- releases
+//
+// A sequence of L tokens whose tokens from the sinks to `gone` have left its window
+// holds the pages [0, S) and [max(S, gone / page), ceil(L / page)) of its row, S the
+// pages of the sinks.  A page goes back when all rows that held it before the call
+// let it go: `holders` counts the rows before, `dropped` those that let go, both
+// by integer atomics, whose order does not show.  Freed pages are pushed by number.
+// `freed` counts them by chunks of pages, so that every block of the last launch
+// knows its place.
+
+struct LArgs {
+  PageRelease r;
+  int *holders, *dropped, *freed;  // workspace
+  int segments;                    // of a row, kSegment entries each
+};
+constexpr int kSegment = 1024;  // entries of a row that a wave walks
+constexpr int kChunk = 4096;    // pages whose freed ones are counted together
+
+struct Held {
+  int end, sinks, first;  // pages of the row: [0, sinks) and [first, end)
+  __device__ inline int count() const { return sinks + max(0, end - first); }
+  __device__ inline int entry(int i) const { return i < sinks ? i : first + i - sinks; }
+  __device__ inline bool has(int j) const { return j < sinks || (j >= first && j < end); }
+};
+__device__ inline Held held(const PageRelease &r, int tokens, int gone) {
+  Held h;
+  h.end = min(pages_of(tokens, r.page_shift), r.max_pages);
+  const int s = pages_of(r.sinks, r.page_shift);
+  h.sinks = min(s, h.end);
+  h.first = max(s, gone >> r.page_shift);
+  return h;
+}
+struct Row {
+  int L, gone;
+};
+__device__ inline Row row_of(const PageRelease &r, int b) {
+  return {max(0, r.seq_len[b]), r.gone ? max(0, r.gone[b]) : 0};
+}
+
+__device__ inline void count_row(const LArgs &a, int b, int segment) {
+  const Row x = row_of(a.r, b);
+  const Held h = held(a.r, x.L, x.gone);
+  const int32_t *row = a.r.table + (size_t)b * a.r.max_pages;
+  const int i1 = min((segment + 1) * kSegment, h.count());
+  bool bad = false;
+  for (int i = segment * kSegment + (threadIdx.x & 63); i < i1; i += 64) {
+    const int id = row[h.entry(i)];
+    if (in_pool(id, a.r.n_pages)) atomicAdd(&a.holders[id], 1);
+    else bad = true;
+  }
+  if (bad && a.r.status) atomicOr(&a.r.status[b], AVTP_FLAG_BAD_PAGE);
+}
+
+__device__ inline int read_now(const int *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+__device__ inline void drop_row(const LArgs &a, int b, int segment) {
+  const PageRelease &r = a.r;
+  const int lane = threadIdx.x & 63, W = r.window;
+  const Row x = row_of(r, b);
+  const int32_t *row = r.table + (size_t)b * r.max_pages;
+  int keep = min(max(0, r.keep_len[b]), x.L), gone = x.gone;
+  bool refused = false;
+  if (keep > 0 && keep < x.L) {
+    // no cut inside a page that others hold, none behind what the window has left
+    const int at = keep >> r.page_shift;
+    const int id = (keep & ((1 << r.page_shift) - 1)) && at < r.max_pages ? row[at] : -1;
+    refused = in_pool(id, r.n_pages) && read_now(&a.holders[id]) > 1;
+    if (x.gone > 0 && (W == 0 || keep - W + 1 < x.gone)) refused = true;
+  }
+  if (refused) keep = x.L;
+  else if (keep == 0) gone = 0;
+  else if (W > 0) gone = max(gone, keep - W + 1);
+  if (segment == 0 && lane == 0) {
+    r.seq_len_out[b] = keep;
+    if (r.gone_out) r.gone_out[b] = gone;
+    if (refused && r.status) atomicOr(&r.status[b], AVTP_FLAG_REFUSED);
+  }
+  const Held h = held(r, x.L, x.gone);
+  const Held after = held(r, keep, gone);
+  const int i1 = min((segment + 1) * kSegment, h.count());
+  for (int i = segment * kSegment + lane; i < i1; i += 64) {
+    const int j = h.entry(i), id = after.has(j) ? -1 : row[j];
+    if (!in_pool(id, r.n_pages)) continue;
+    if (atomicAdd(&a.dropped[id], 1) + 1 == read_now(&a.holders[id])) atomicAdd(&a.freed[id / kChunk], 1);
+  }
+}
+
+// THREADS threads push the freed pages [p0, p0 + kChunk) from place `at` on.
+template <int THREADS>
+__device__ inline int push_chunk(const LArgs &a, int p0, int at, int *wsum) {
+  constexpr int PER = kChunk / THREADS, WAVES = THREADS / 64;
+  const int tid = threadIdx.x, wave = tid >> 6;
+  uint32_t mine = 0;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int p = p0 + tid * PER + i;
+    if (p >= a.r.n_pages) break;
+    const int n = read_now(&a.holders[p]);
+    mine |= (n > 0 && read_now(&a.dropped[p]) == n ? 1u : 0u) << i;
+  }
+  const int n = __builtin_popcount(mine);
+  const int incl = (int)wave::prefix_sum((uint32_t)n);
+  __syncthreads();
+  if ((tid & 63) == 63) wsum[wave] = incl;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < wave) at += wsum[w];
+    total += wsum[w];
+  }
+  at += incl - n;
+#pragma unroll
+  for (int i = 0; i < PER; ++i)
+    if (mine >> i & 1) {
+      if (at < a.r.n_pages) a.r.free_pages[at] = p0 + tid * PER + i;
+      ++at;
+    }
+  return total;
+}
+__device__ inline int stack_of(const PageRelease &r) { return min(max(0, r.free_count[0]), r.n_pages); }
+
+// holders, dropped and freed lie in one piece
+__global__ __launch_bounds__(kThreads) void page_release_clear_kernel(int *ws, long long n) {
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) ws[i] = 0;
+}
+__global__ __launch_bounds__(kThreads) void page_release_count_kernel(LArgs a) {
+  const int w = blockIdx.x * kWaves + (threadIdx.x >> 6), b = w / a.segments;
+  if (b < a.r.B) count_row(a, b, w % a.segments);
+}
+__global__ __launch_bounds__(kThreads) void page_release_drop_kernel(LArgs a) {
+  const int w = blockIdx.x * kWaves + (threadIdx.x >> 6), b = w / a.segments;
+  if (b < a.r.B) drop_row(a, b, w % a.segments);
+}
+__global__ __launch_bounds__(kThreads) void page_release_push_kernel(LArgs a) {
+  __shared__ int wsum[kWaves];
+  int sum = 0;
+  for (int i = threadIdx.x; i < (int)blockIdx.x; i += kThreads) sum += a.freed[i];
+  const int at = stack_of(a.r) + block_sum<kWaves>(sum, wsum);
+  const int n = push_chunk<kThreads>(a, blockIdx.x * kChunk, at, wsum);
+  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) a.r.free_count_out[0] = min(at + n, a.r.n_pages);
+}
+
+}  // namespace
+
+hipError_t launch_page_fork(hipStream_t st, const PageFork &F) {
+  clear_pending_error();
+  // four sequences a block (one per wave) up to 1,024 blocks, at most 64 (one per lane)
+  int per = (F.B + 1023) / 1024;
+  static_assert(AVTP_MAX_REQUESTS / 1024 <= 64, "a lane per sequence of a block");
+  per = per < kWaves ? kWaves : per;
+  const FArgs a{F, per};
+  hipLaunchKernelGGL(page_fork_kernel, dim3((unsigned)((F.B + per - 1) / per)), dim3(kThreads), 0, st, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_page_copy(hipStream_t st, const avtp_pages &P, const int32_t *src_page,
+                            const int32_t *dst_page, int64_t n) {
+  clear_pending_error();
+  CArgs a;
+  a.k = (char *)P.k;
+  a.v = (char *)P.v;
+  a.src = src_page;
+  a.dst = dst_page;
+  a.page_bytes = (long long)P.Hkv * P.page_size * P.d * (P.dtype == AVTP_FP32 ? 4 : 2);
+  constexpr int kBytes = kThreads * kUnits * 16;
+  a.chunks = (int)((a.page_bytes + kBytes - 1) / kBytes);
+  a.n_pages = P.n_pages;
+  // (blocks of 256 threads, fewer than 2^24 in a launch)
+  const int64_t most = ((1 << 24) - 1) / (2 * a.chunks);
+  for (int64_t i = 0; i < n; i += most) {
+    const int64_t m = n - i < most ? n - i : most;
+    hipLaunchKernelGGL(page_copy_kernel, dim3((unsigned)(m * 2 * a.chunks)), dim3(kThreads), 0, st, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    a.src += m;
+    a.dst += m;
+  }
+  return hipSuccess;
+}
+
+size_t page_release_workspace_bytes(int n_pages) {
+  return 4 * (2 * (size_t)n_pages + ((size_t)n_pages + kChunk - 1) / kChunk);
+}
+
+hipError_t launch_page_release(hipStream_t st, const PageRelease &R, int32_t *ws) {
+  clear_pending_error();
+  LArgs a;
+  a.r = R;
+  a.holders = ws;
+  a.dropped = ws + R.n_pages;
+  a.freed = ws + 2 * (size_t)R.n_pages;
+  a.segments = (R.max_pages + kSegment - 1) / kSegment;
+  const long long words = (long long)page_release_workspace_bytes(R.n_pages) / 4;
+  const long long waves = (long long)R.B * a.segments;
+  const dim3 rows((unsigned)((waves + kWaves - 1) / kWaves));
+  hipLaunchKernelGGL(page_release_clear_kernel, dim3((unsigned)((words + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                     st, ws, words);
+  hipLaunchKernelGGL(page_release_count_kernel, rows, dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(page_release_drop_kernel, rows, dim3(kThreads), 0, st, a);
+  hipLaunchKernelGGL(page_release_push_kernel, dim3((unsigned)((R.n_pages + kChunk - 1) / kChunk)), dim3(kThreads), 0,
+                     st, a);
+  return hipGetLastError();
+}
+
+}  // namespace avtp

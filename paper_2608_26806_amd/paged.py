@@ -12,6 +12,15 @@ stack of free pages, and each layer's pages.
     out, lse = cache.attend(layer, q, cu_q, scale)     # new tokens over the cache
     cache.trim(keep_len)                               # requests that ended, drafts taken back
 
+A layer whose queries and keys are still to be normalised and rotated stores
+and turns them in one call, and sequences may start from others' tokens:
+
+    q = cache.store_rotary(layer, rotary, pos, q, k, v, q_weight=wq, k_weight=wk)
+    cache.fork(parent, fork_len)                       # more questions about the same images
+
+With a ``window`` (and ``sinks``) every ``attend`` sees the latest tokens and the
+first ones only, and ``trim`` also hands back the pages of what has left the window.
+
 Every step runs in libavtp.so on torch's current stream (torch copies the new
 lengths over the old ones); nothing is read back to the host, and the state
 lies in buffers that stay where they are, so the calls of a decode step can be
@@ -30,17 +39,31 @@ from . import avtp as A
 
 class PagedCache:
     """Pages of ``layers`` layers for ``requests`` sequences of at most
-    ``max_pages`` pages each, out of ``n_pages`` in all."""
+    ``max_pages`` pages each, out of ``n_pages`` in all.
+
+    ``sharing``: sequences may be forked; ``trim`` then hands a page back when no
+    sequence holds it any more.  ``window``, ``sinks``: what attention sees (this
+    implies sharing; a row of the table still counts all of a sequence's tokens)."""
 
     def __init__(self, requests: int, n_pages: int, max_pages: int, Hkv: int, d: int,
-                 page_size: int = 64, layers: int = 1, dtype=torch.bfloat16, device="cuda"):
+                 page_size: int = 64, layers: int = 1, dtype=torch.bfloat16, device="cuda",
+                 sharing: bool = False, window: Optional[int] = None, sinks: int = 0):
+        if (window is not None and window < 1) or sinks < 0 or (window is None and sinks):
+            raise ValueError("a window of 1 or more, and sinks of 0 or more with it, are needed")
         self.page_size = page_size
+        self.window, self.sinks = window, sinks
+        self.sharing = sharing or window is not None
         self.layers = [A.Pages.empty(n_pages, Hkv, page_size, d, dtype, device) for _ in range(layers)]
         ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)  # noqa: E731
         # lengths and the number of free pages side by side: one copy takes a
         # call's results over
         self._state, self._after = ints(requests + 1), ints(requests + 1)
         self.seq_len, self.free_count = self._state[:requests], self._state[requests:]
+        if self.sharing:
+            # tokens that have left each sequence's window, and scratch
+            self.gone, self._gone_after = ints(requests), ints(requests)
+            self._src, self._dst = ints(requests), ints(requests)
+            self._ws = A.alloc_workspace(A.page_release_workspace_bytes(n_pages), device)
         # the lengths as attention takes them: 0 for requests whose last new tokens
         # got no place, so that their queries see nothing
         self._seen = ints(requests)
@@ -75,6 +98,40 @@ class PagedCache:
             raise ValueError("no tokens have been reserved")
         A.page_store(self.layers[layer], k, v, slot_map, keep_idx)
 
+    def store_rotary(self, layer: int, rotary, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                     v: torch.Tensor, q_weight: Optional[torch.Tensor] = None,
+                     k_weight: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                     slot_map: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """A layer's queries and keys of the tokens reserved last, normalised head
+        by head (where a weight is given) and rotated by their positions (a
+        ``Rotary``; pos [planes, N] or [N]); K and V go into the pages, the queries
+        are returned."""
+        if slot_map is None:
+            slot_map = self.slots
+        if slot_map is None:
+            raise ValueError("no tokens have been reserved")
+        return A.page_store_rotary(self.layers[layer], rotary, pos, q, k, v, slot_map, q_weight, k_weight, eps)
+
+    def fork(self, parent: torch.Tensor, fork_len: Optional[torch.Tensor] = None,
+             status: Optional[torch.Tensor] = None) -> None:
+        """Every empty sequence b with parent[b] >= 0 gets the first fork_len[b] tokens
+        of that sequence (all of them without a fork_len): their whole pages are shared, a
+        last one filled in part is copied in every layer.  One that cannot be forked stays
+        empty and flags FLAG_REFUSED, or FLAG_NO_PAGES, in ``status`` [B]."""
+        if not self.sharing:
+            raise ValueError("a cache made with sharing=True is needed")
+        B = self.seq_len.numel()
+        if fork_len is None:
+            fork_len = self.seq_len[parent.clamp(min=0, max=B - 1).long()]
+        A.prepare_page_fork(self.page_size, parent, fork_len, self.seq_len, self.free_pages, self.free_count,
+                            self.block_table, self._after[:B], self._after[B:], self._src, self._dst,
+                            self.gone, self._gone_after, status)()
+        for pages in self.layers:
+            A.page_copy(pages, self._src, self._dst)
+        # (attention takes a fork's tokens from its next reservation on)
+        self._state.copy_(self._after)
+        self.gone.copy_(self._gone_after)
+
     def attend(self, layer: int, q: torch.Tensor, cu_q: torch.Tensor, softmax_scale: float,
                max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
                lse: Optional[torch.Tensor] = None, status: Optional[torch.Tensor] = None,
@@ -83,11 +140,23 @@ class PagedCache:
         K and V are stored) over the layer's pages; returns (out, lse).  Queries
         of a request that got no place for them: out 0, lse -inf."""
         return A.page_attention(self.layers[layer], q, cu_q, self._seen, self.block_table,
-                                softmax_scale, max_kv_len, out, lse, status, ws)
+                                softmax_scale, max_kv_len, out, lse, status, ws, window=self.window,
+                                sinks=self.sinks)
 
     def trim(self, keep_len: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
-        """Cut every sequence to its first keep_len tokens (0: it has ended)."""
+        """Cut every sequence to its first keep_len tokens (0: it has ended), and with a
+        window let go of what has left it.  With sharing, a cut inside a page that
+        another sequence holds, or behind what the window has left, is refused: the
+        sequence stays whole and flags FLAG_REFUSED in ``status`` [B]."""
         B = self.seq_len.numel()
+        if self.sharing:
+            A.prepare_page_release(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
+                                   self.free_count, self._after[:B], self._after[B:], self._ws, self.window or 0,
+                                   self.sinks, self.gone, self._gone_after, status)()
+            torch.minimum(self._seen, self._after[:B], out=self._seen)
+            self._state.copy_(self._after)
+            self.gone.copy_(self._gone_after)
+            return
         A.prepare_page_trim(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
                             self.free_count, self._after[:B], self._after[B:], status)()
         torch.minimum(self._seen, self._after[:B], out=self._seen)

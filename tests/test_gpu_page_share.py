@@ -1,0 +1,289 @@
+"""Forks, page copies and releases against the oracle: whole numbers and copies,
+equal bit for bit."""
+import numpy as np
+import pytest
+import torch
+
+from gpu_util import need_gpu, say, to_host_bits
+from oracle import pages as P
+from paper_2608_26806_amd import avtp as A
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    need_gpu()
+    A.lib()
+
+
+def ints(x):
+    return torch.tensor(np.asarray(x, dtype=np.int64).astype(np.int32), device="cuda")
+
+
+def host(t):
+    return t.cpu().numpy().astype(np.int64)
+
+
+class Pool:
+    """Requests with pages in no order; `free`: pages on the stack."""
+
+    def __init__(self, seed, lens, ps, free):
+        rng = np.random.default_rng(seed)
+        self.ps, self.lens = ps, np.asarray(lens)
+        need = [-(-int(n) // ps) for n in lens]
+        self.n_pages = sum(need) + free
+        order = rng.permutation(self.n_pages)
+        self.table = np.full((len(lens), max(1, max(need)) + 2), -1)
+        at = 0
+        for b, n in enumerate(need):
+            self.table[b, :n] = order[at:at + n]
+            at += n
+        self.free = np.concatenate([order[at:], np.full(at, -1)])
+        self.count = free
+
+    def fork(self, parent, n, gone=None, count=None):
+        count = self.count if count is None else count
+        say(f"[fork] {len(parent)} sequences, pages of {self.ps}")
+        want = P.page_fork(self.ps, parent, n, self.lens, self.free, count, self.table, gone)
+        B = len(parent)
+        table, status = ints(self.table), torch.zeros(B, dtype=torch.int32, device="cuda")
+        out = [torch.full((m,), -7, dtype=torch.int32, device="cuda") for m in (B, 1, B, B)]
+        left = None if gone is None else torch.full((B,), -7, dtype=torch.int32, device="cuda")
+        A.prepare_page_fork(self.ps, ints(parent), ints(n), ints(self.lens), ints(self.free), ints([count]), table, *out,
+                            None if gone is None else ints(gone), left, status)()
+        got = [host(table), host(out[0]), int(out[1]), host(out[2]), host(out[3]), None if left is None else host(left),
+               host(status)]
+        for g, w, name in zip(got, want, ("table", "seq_len", "free_count", "src", "dst", "gone", "flags")):
+            assert np.array_equal(g, w), name
+        return got
+
+    def release(self, keep, window=0, sinks=0, gone=None, count=None):
+        count = self.count if count is None else count
+        say(f"[release] {len(keep)} sequences, pages of {self.ps}, window {window}, sinks {sinks}")
+        want = P.page_release(self.ps, keep, self.lens, self.table, self.free, count, window, sinks, gone)
+        free, status = ints(self.free), torch.zeros(len(keep), dtype=torch.int32, device="cuda")
+        got = A.page_release(self.ps, ints(keep), ints(self.lens), ints(self.table), free, ints([count]), window, sinks,
+                             None if gone is None else ints(gone), status)
+        got = [host(free), host(got[0]), int(got[1]), None if gone is None else host(got[2]), host(status)]
+        for g, w, name in zip(got, want, ("free_pages", "seq_len", "free_count", "gone", "flags")):
+            assert g is None or np.array_equal(g, w), name
+        return got
+
+
+def families(seed, n, size, ps, longest, own):
+    """A pool in which each prompt's whole pages are shared by size - 1 more rows."""
+    rng = np.random.default_rng(seed)
+    prompt = np.repeat(rng.integers(0, longest, n), size)
+    first = np.arange(n * size) // size * size
+    child = np.arange(n * size) != first
+    tails = rng.integers(0, own, n * size)
+    lens = np.where(child, prompt + tails, prompt)
+    pool = Pool(seed, lens, ps, 5)
+    for b in np.nonzero(child)[0]:
+        w = int(prompt[b]) // ps
+        pool.table[b, :w] = pool.table[first[b], :w]
+    return pool, rng
+
+
+@pytest.mark.parametrize("ps", [16, 64, 1024])
+@pytest.mark.parametrize("B", [1, 2, 7, 65, 1500])
+def test_forks(B, ps):
+    rng = np.random.default_rng(B + ps)
+    for t in range(4):
+        child = rng.random(B) < (0.0 if B == 1 else 0.6)
+        child[0] = False
+        lens = np.where(child, 0, rng.integers(0, 5 * ps, B))
+        pool = Pool(B + t, lens, ps, [0, 1, B // 3, B][t])
+        parents = np.nonzero(~child)[0]
+        parent = np.where(child & (rng.random(B) < 0.9), rng.choice(parents, B), -1)
+        n = np.array([int(rng.choice([0, ps, lens[p] // ps * ps, lens[p], rng.integers(0, lens[p] + 1)])) if p >= 0 else 9
+                      for p in parent])
+        n = np.minimum(n, np.where(parent >= 0, lens[np.maximum(parent, 0)], n))
+        pool.fork(parent, n)
+
+
+def test_forks_that_cannot_be_made():
+    ps = 16
+    pool = Pool(1, [40, 0, 0, 0, 0, 0, 50, 0], ps, 10)
+    #        itself no  past the end  negative  of a fork  not empty  no row  more than the batch
+    parent = [-1, 0, 0, 0, 1, 5, 0, 99]
+    n = [0, 40, 41, -1, 3, 0, 10, 0]
+    _, lens, count, src, dst, _, flags = pool.fork(parent, n)
+    assert flags.tolist() == [0, 0, 64, 64, 64, 64, 64, 64] and lens.tolist() == [40, 40, 0, 0, 0, 0, 50, 0]
+    assert count == 9 and (src[1], dst[1]) == (pool.table[0, 2], pool.free[9])
+
+
+def test_forks_behind_a_window():
+    pool = Pool(2, [100, 0, 0, 90, 0], 16, 4)
+    gone = [37, 0, 5, 0, 0]
+    got = pool.fork([-1, 0, 0, -1, 3], [0, 100, 99, 0, 20], gone)
+    assert got[5].tolist() == [37, 37, 5, 0, 0] and got[6].tolist() == [0, 0, 64, 0, 0]
+
+
+def test_forks_without_pages():
+    pool = Pool(3, [100, 0, 0, 0, 0], 16, 4)
+    got = pool.fork([-1, 0, 0, 0, 0], [0, 17, 33, 32, 50], count=1)
+    assert got[6].tolist() == [0, 0, 32, 0, 32] and got[1].tolist() == [100, 17, 0, 32, 0] and got[2] == 0
+    # entries outside the pool: of the page to be copied, and of the stack
+    pool.table[0, 1] = -5
+    assert pool.fork([-1, 0, 0, -1, -1], [0, 17, 33, 0, 0])[6].tolist() == [0, 16, 0, 0, 0]
+    pool.free[3] = 10 ** 6
+    pool.fork([-1, 0, 0, -1, -1], [0, 37, 33, 0, 0])
+
+
+@pytest.mark.parametrize("dtype, Hkv, d, ps", [(torch.bfloat16, 1, 64, 16), (torch.bfloat16, 8, 128, 16), (torch.float32, 3, 64, 128),
+                                            (torch.bfloat16, 5, 128, 1024)])
+def test_copies(dtype, Hkv, d, ps):
+    for n in (0, 1, 5, 40):
+        gen = torch.Generator(device="cuda").manual_seed(n)
+        n_pages = 2 * n + 3
+        bits = torch.int16 if dtype == torch.bfloat16 else torch.int32
+        info = torch.iinfo(bits)
+        pages = A.Pages(*(torch.randint(info.min, info.max, (n_pages, Hkv, ps, d), generator=gen, device="cuda", dtype=bits)
+                          .view(dtype) for _ in range(2)))
+        order = torch.randperm(n_pages, generator=gen, device="cuda").to(torch.int32)
+        src, dst = order[:n].clone(), order[n:2 * n].clone()
+        if n > 4:
+            src[1], dst[2], src[3], dst[3], dst[4] = -1, -1, n_pages, 0x7FFFFFFF, -2 ** 31
+        want = [P.page_copy(to_host_bits(t.view(bits)), host(src), host(dst)) for t in (pages.k, pages.v)]
+        A.page_copy(pages, src, dst)
+        for t, w in zip((pages.k, pages.v), want):
+            assert np.array_equal(to_host_bits(t.view(bits)), w)
+
+
+def test_one_source_many_copies():
+    pages = A.Pages(*(torch.randn(9, 2, 16, 64, device="cuda").bfloat16() for _ in range(2)))
+    k = pages.k.clone()
+    A.page_copy(pages, ints([3] * 6), ints([0, 1, 2, 4, 5, 8]))
+    for i in range(9):
+        assert torch.equal(pages.k[i], k[i if i in (6, 7) else 3])
+
+
+@pytest.mark.parametrize("ps", [16, 128])
+@pytest.mark.parametrize("B", [1, 5, 64, 300])
+def test_releases_of_whole_sequences_and_cuts(B, ps):
+    for t in range(3):
+        rng = np.random.default_rng(B + t)
+        lens = rng.integers(0, 7 * ps, B)
+        pool = Pool(B + t, lens, ps, [0, 3, 50][t])
+        keep = np.where(rng.random(B) < 0.3, 0, np.maximum(0, lens - rng.integers(-3, 3 * ps, B)))
+        got = pool.release(keep)
+        assert not got[4].any()
+        # what trim does, in another order
+        free, lens_out, count, _ = P.page_trim(ps, keep, lens, pool.table, pool.free, pool.count)
+        assert count == got[2] and np.array_equal(lens_out, got[1])
+        assert set(free[:count].tolist()) == set(got[0][:count].tolist())
+
+
+@pytest.mark.parametrize("n, size, ps, longest", [(1, 2, 16, 100), (8, 8, 16, 900), (40, 4, 64, 2000), (3, 100, 16, 4000)])
+def test_releases_of_shared_pages(n, size, ps, longest):
+    for t in range(4):
+        pool, rng = families(n + t, n, size, ps, longest, 5 * ps)
+        B = n * size
+        ended = rng.random(B) < [0.2, 0.7, 1.0, 0.5][t]
+        keep = np.where(ended, 0, np.maximum(0, pool.lens - rng.integers(0, 3 * ps, B)))
+        got = pool.release(keep)
+        if t == 2:                                   # all have ended: every page is back
+            assert got[2] == len({int(i) for b in range(B) for i in pool.table[b, :-(-int(pool.lens[b]) // ps)]}) + pool.count
+
+
+def test_a_cut_in_a_shared_page_is_refused():
+    pool = Pool(5, [64, 100, 100], 16, 3)
+    pool.table[1, :4] = pool.table[0, :4]
+    # 40: inside a shared page; 48: at the end of one; 70: inside an own one
+    for keep, flags in (([64, 40, 100], [0, 64, 0]), ([64, 48, 100], [0, 0, 0]), ([64, 70, 100], [0, 0, 0]),
+                        ([0, 40, 100], [0, 64, 0]), ([40, 0, 100], [64, 0, 0]), ([40, 40, 40], [64, 64, 0])):
+        got = pool.release(keep)
+        assert got[4].tolist() == flags
+        assert got[1].tolist() == [L if f else k for k, L, f in zip(keep, pool.lens, flags)]
+
+
+@pytest.mark.parametrize("window, sinks", [(1, 0), (16, 1), (100, 4), (33, 70), (1 << 20, 4)])
+@pytest.mark.parametrize("ps", [16, 64])
+def test_releases_behind_a_window(ps, window, sinks):
+    rng = np.random.default_rng(window + ps)
+    for B in (1, 9, 200):
+        lens = rng.integers(0, 40 * ps, B)
+        pool = Pool(B, lens, ps, 4)
+        keep = np.where(rng.random(B) < 0.1, 0, lens)
+        first = pool.release(keep, window, sinks, np.zeros(B, dtype=int))
+        # the next step: a few tokens further on, the pages that left are others' now
+        pool.free, pool.count = first[0], first[2]
+        gone = first[3]
+        for b in range(B):
+            hole = slice(-(-sinks // ps), max(-(-sinks // ps), int(gone[b]) // ps))
+            pool.table[b, hole] = rng.integers(-3, pool.n_pages, len(pool.table[b, hole]))
+        room = pool.table.shape[1] * ps
+        more = np.where(first[1] > 0, rng.integers(0, 2 * ps, B), 0)
+        lens2 = np.minimum(first[1] + more, room)
+        for b in range(B):                           # pages for them
+            for j in range(-(-int(first[1][b]) // ps), -(-int(lens2[b]) // ps)):
+                if pool.count > 0:
+                    pool.count -= 1
+                    pool.table[b, j] = pool.free[pool.count]
+                else:
+                    lens2[b] = min(lens2[b], j * ps)
+        pool.lens = lens2
+        back = np.where(rng.random(B) < 0.3, rng.integers(1, 4, B), 0)
+        pool.release(np.maximum(0, lens2 - back), window, sinks, gone)
+        pool.release(lens2, 0, sinks, gone)
+
+
+def test_a_cut_behind_the_window_is_refused():
+    pool = Pool(6, [200, 200, 200, 200], 16, 3)
+    gone = [101, 101, 101, 0]
+    got = pool.release([200, 199, 0, 50], 100, 4, gone)
+    assert got[4].tolist() == [0, 64, 0, 0] and got[3].tolist() == [101, 101, 0, 0]
+
+
+def test_odd_tables():
+    # entries outside the pool, a row with a page twice, lengths past the table, a stack that claims too much
+    pool = Pool(7, [100, 60, 200], 16, 3)
+    pool.table = pool.table[:, :9].copy()
+    pool.table[0, 2], pool.table[0, 3] = -1, 10 ** 6
+    pool.table[1, 1] = pool.table[1, 0]
+    pool.release([0, 60, 144])
+    pool.release([0, 0, 0])
+    pool.release([100, 16, 200])
+    free, status = ints(pool.free), torch.zeros(3, dtype=torch.int32, device="cuda")
+    got = A.page_release(16, ints([0, 0, 0]), ints([100, 60, 200]), ints(pool.table), free, ints([10 ** 9]), status=status)
+    assert int(got[1]) == pool.n_pages and np.array_equal(host(free), pool.free)
+
+
+def test_releases_of_long_rows_and_many_pages():
+    rng = np.random.default_rng(8)
+    lens = [16 * 5000 + 3, 0, 16 * 1024, 16 * 1025 - 1]
+    pool = Pool(8, lens, 16, 10)
+    pool.release([7, 0, 0, 16 * 1025 - 1])
+    pool.release([16 * 5000, 0, 16 * 1024, 5], 300, 20, np.zeros(4, dtype=int))
+    lens = rng.integers(0, 16 * 200, 300)
+    pool = Pool(9, lens, 16, 20000)
+    pool.release(np.where(rng.random(300) < 0.5, 0, lens))
+
+
+def test_graph():
+    pool, rng = families(11, 8, 4, 16, 500, 80)
+    B = 32
+    keep, lens, table, free, count = ints(pool.lens), ints(pool.lens), ints(pool.table), ints(pool.free), ints([pool.count])
+    out = [torch.empty(m, dtype=torch.int32, device="cuda") for m in (B, 1)]
+    ws = A.alloc_workspace(A.page_release_workspace_bytes(pool.n_pages))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    call = A.prepare_page_release(16, keep, lens, table, free, count, *out, ws, stream=side)
+    with torch.cuda.stream(side):
+        call()
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call()
+    torch.cuda.current_stream().wait_stream(side)
+    for i in range(4):
+        k = np.where(rng.random(B) < 0.4, 0, pool.lens)
+        keep.copy_(ints(k))
+        free.copy_(ints(pool.free))
+        ws.random_(0, 255)                            # the workspace needs no clearing
+        g.replay()
+        torch.cuda.synchronize()
+        want = P.page_release(16, k, pool.lens, pool.table, pool.free, pool.count)
+        assert np.array_equal(host(free), want[0]) and np.array_equal(host(out[0]), want[1]) and int(out[1]) == want[2]
