@@ -182,6 +182,7 @@ struct PageAttnPlan {
   bool few;        // tiles of one wave's rows
   int tile;        // rows of a tile: 16 or 32 (few), 128
   bool brief;      // short work: a block per tile, nothing cut
+  bool half;       // brief: blocks of two waves instead of four
   int64_t blocks;  // few: workers that share the work evenly; many: a tile's key range each
   int nsplit;      // many: key ranges per tile
   int least;       // few: units (32 keys of a tile) per worker, at least

@@ -876,10 +876,10 @@ __device__ inline int tile_of_rank(const KArgs &a, int rank, int &b, Seq &s) {
 // Short work: a block takes a whole tile, its W waves a share of the
 // keys each, and joins their parts in LDS: no second launch.
 constexpr int kShortWaves = 4;  // whose buffers a CU's LDS holds
-template <typename T, int D, int M, typename A>
-__global__ __launch_bounds__(64 * kShortWaves) void page_attn_short_kernel(A a) {
+template <typename T, int D, int M, int W, typename A>
+__global__ __launch_bounds__(64 * W) void page_attn_short_kernel(A a) {
   using S_ = Shape<T, D, M, 1, 1>;
-  constexpr int KS = S_::KS, BUF = 2 * S_::TB, W = kShortWaves;
+  constexpr int KS = S_::KS, BUF = 2 * S_::TB;
   static_assert(M * D * 4 <= BUF, "a part fits a stage buffer");
   __shared__ __attribute__((aligned(16))) char smA[W * BUF];
   __shared__ __attribute__((aligned(16))) char smB[W * BUF];
@@ -1080,7 +1080,9 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // (longer sequences run all the same)
   max_kv_len = max_kv_len < 1 ? 1 : max_kv_len < (1 << 30) ? max_kv_len : (1 << 30);
   // what a row sees (a tile's first rows see a few more keys than its last)
-  if (w.window > 0 && max_kv_len > (int64_t)w.window + w.sinks) max_kv_len = (int64_t)w.window + w.sinks;
+  const int64_t seen = (int64_t)w.window + w.sinks;
+  const bool alike = w.window > 0 && max_kv_len >= 2 * seen;
+  if (w.window > 0 && max_kv_len > seen) max_kv_len = seen;
   const int64_t rows = N_q * (Hq / P.Hkv);
   // one wave of 16 or 32 rows for a sequence, or blocks of 128; a tile's ranks: at most
   auto tiles_of = [&](int bm) { return (rows / bm + B) * P.Hkv; };
@@ -1088,6 +1090,29 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   const int64_t brief = tiles_of(small);
   L.brief = P.dtype == AVTP_BF16 && brief <= (P.d == 64 ? kShortTiles64 : kShortTiles) &&
             max_kv_len <= (small == 32 && brief >= kShortFull ? kShortFullKeys : kShortKeys);
+  // Behind a window most sequences see equally much (told by a bound of twice the window
+  // or more), so that blocks of single tokens end together: four waves or two a tile, where
+  // they are on half of the CUs in one round or fill 0.7 of the places of several.  One
+  // token, 32/8 heads of 128, window 1,024, the line against blocks: 8 requests (64
+  // tiles) 16.8 / 17.0 us, 16 22.9 / 19.0, 32 33.4 / 28.4, 48 44.3 / 39.5 (two waves;
+  // four 46.7), 64 of which some are short 49.6 / 44.7, 80 65.8 / 62.2 (two 67.7), 96 76.2
+  // / 69.1 (two 71.7), 128 97.5 / 87.8; window 256, 64 24.3 / 24.4 (four 34.5), 96 29.4 /
+  // 25.6 (four 30.9); window 3,000, 8 26.6 / 35.9, 40 86.6 / 88.4, 80 (two 0.63 full) 164 /
+  // 181, 96 194 / 182; 16/16 heads of 64, window 1,024, 8 (128 tiles) 17.5 / 14.1.
+  if (alike && !L.brief && P.dtype == AVTP_BF16 && small == 16) {
+    const int64_t now = ((rows + 15) / 16 > B ? (rows + 15) / 16 : B) * P.Hkv;
+    // the part of their places that the blocks of the last round and those before fill
+    auto fill = [&](int waves) {
+      const int64_t places = 1024 / waves * (P.d == 64 ? 2 : 1), rounds = (now + places - 1) / places;
+      const double f = (double)now / (double)(rounds * places);
+      return (rounds == 1 ? now >= 128 : f >= 0.7) ? f : 0.;
+    };
+    const double four = fill(kShortWaves), two = fill(kShortWaves / 2);
+    const bool once = now <= 256 * (P.d == 64 ? 2 : 1);
+    L.half = !(four > 0 && (once || (max_kv_len > 512 && four > 1.12 * two)));
+    L.brief = four > 0 || two > 0;
+    if (L.half && two == 0.) L.brief = false;
+  }
   // Up to 32 rows a sequence is one tile of the even line; more rows read its keys once
   // per 32 there and once per 128 in a block.  us, line against blocks: 28/4 heads, 64
   // requests of 300-16,000 keys, 4 tokens (28 rows) 102 / 292, 5 (35 rows) 183 / 294, 9 (63)
@@ -1159,8 +1184,14 @@ static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const A &k) {
   const dim3 grid((unsigned)L.blocks);
   if constexpr (sizeof(T) == 2) {
     if (L.brief) {
-      if (L.tile == 16) hipLaunchKernelGGL((page_attn_short_kernel<T, D, 16, A>), grid, dim3(64 * kShortWaves), 0, st, k);
-      else hipLaunchKernelGGL((page_attn_short_kernel<T, D, 32, A>), grid, dim3(64 * kShortWaves), 0, st, k);
+      auto run = [&](auto m_tag, auto w_tag) {
+        constexpr int M = decltype(m_tag)::value, W = decltype(w_tag)::value;
+        hipLaunchKernelGGL((page_attn_short_kernel<T, D, M, W, A>), grid, dim3(64 * W), 0, st, k);
+      };
+      constexpr std::integral_constant<int, kShortWaves> all{};
+      if (L.tile == 32) run(std::integral_constant<int, 32>{}, all);
+      else if (!A::WIN || !L.half) run(std::integral_constant<int, 16>{}, all);
+      else if constexpr (A::WIN) run(std::integral_constant<int, 16>{}, std::integral_constant<int, kShortWaves / 2>{});
       return hipGetLastError();
     }
   }

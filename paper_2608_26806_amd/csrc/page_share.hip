@@ -90,7 +90,15 @@ __global__ __launch_bounds__(kThreads) void page_fork_kernel(FArgs x) {
     const int whole = len >> a.page_shift, fresh = __builtin_amdgcn_readlane(dst, j);
     const int32_t *from = a.table + (size_t)parent * a.max_pages;
     int32_t *to = a.table + (size_t)(b0 + j) * a.max_pages;
-    for (int i = lane; i < whole; i += 64) to[i] = from[i];
+    constexpr int U = 8;  // entries in flight
+    for (int i = lane; i < whole; i += 64 * U) {
+      int32_t x[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) x[u] = from[min(i + 64 * u, whole - 1)];
+#pragma unroll
+      for (int u = 0; u < U; ++u)
+        if (i + 64 * u < whole) to[i + 64 * u] = x[u];
+    }
     if (lane == 0 && __builtin_amdgcn_readlane(f.need, j)) to[whole] = fresh;
   }
   if (wave == 0 && b < b1) {
@@ -115,22 +123,14 @@ struct CArgs {
   long long page_bytes;
   int chunks, n_pages;  // chunks of a page, blocks of one page and tensor
 };
-constexpr int kUnits = 4;  // of 16 bytes, per thread
 __global__ __launch_bounds__(kThreads) void page_copy_kernel(CArgs a) {
   const unsigned i = blockIdx.x / (2 * a.chunks), part = blockIdx.x % (2 * a.chunks);
   const int src = a.src[i], dst = a.dst[i];
   if (!in_pool(src, a.n_pages) || !in_pool(dst, a.n_pages)) return;
   char *base = part & 1 ? a.v : a.k;
-  const uint4 *from = reinterpret_cast<const uint4 *>(base + src * a.page_bytes);
-  uint4 *to = reinterpret_cast<uint4 *>(base + dst * a.page_bytes);
-  const int units = (int)(a.page_bytes / 16), u0 = (int)(part >> 1) * kThreads * kUnits + threadIdx.x;
-  uint4 x[kUnits];
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u)
-    if (u0 + u * kThreads < units) x[u] = from[u0 + u * kThreads];
-#pragma unroll
-  for (int u = 0; u < kUnits; ++u)
-    if (u0 + u * kThreads < units) to[u0 + u * kThreads] = x[u];
+  const int u = (int)(part >> 1) * kThreads + threadIdx.x;
+  if (u < (int)(a.page_bytes / 16))
+    reinterpret_cast<uint4 *>(base + dst * a.page_bytes)[u] = reinterpret_cast<const uint4 *>(base + src * a.page_bytes)[u];
 }
 
 // ---- releases
@@ -148,8 +148,9 @@ struct LArgs {
   int *holders, *dropped, *freed;  // workspace
   int segments;                    // of a row, kSegment entries each
 };
-constexpr int kSegment = 1024;  // entries of a row that a wave walks
-constexpr int kChunk = 4096;    // pages whose freed ones are counted together
+constexpr int kPer = 4;                  // entries of a row per lane, their loads in flight together
+constexpr int kSegment = 64 * kPer;      // and of a wave
+constexpr int kChunk = kThreads * 4;     // pages whose freed ones are counted together
 
 struct Held {
   int end, sinks, first;  // pages of the row: [0, sinks) and [first, end)
@@ -176,17 +177,19 @@ __device__ inline void count_row(const LArgs &a, int b, int segment) {
   const Row x = row_of(a.r, b);
   const Held h = held(a.r, x.L, x.gone);
   const int32_t *row = a.r.table + (size_t)b * a.r.max_pages;
-  const int i1 = min((segment + 1) * kSegment, h.count());
+  const int n = h.count(), i0 = segment * kSegment + (threadIdx.x & 63);
+  int id[kPer];
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) id[u] = i0 + u * 64 < n ? row[h.entry(i0 + u * 64)] : 0;
   bool bad = false;
-  for (int i = segment * kSegment + (threadIdx.x & 63); i < i1; i += 64) {
-    const int id = row[h.entry(i)];
-    if (in_pool(id, a.r.n_pages)) atomicAdd(&a.holders[id], 1);
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    if (i0 + u * 64 >= n) break;
+    if (in_pool(id[u], a.r.n_pages)) atomicAdd(&a.holders[id[u]], 1);
     else bad = true;
   }
   if (bad && a.r.status) atomicOr(&a.r.status[b], AVTP_FLAG_BAD_PAGE);
 }
-
-__device__ inline int read_now(const int *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 __device__ inline void drop_row(const LArgs &a, int b, int segment) {
   const PageRelease &r = a.r;
@@ -199,7 +202,7 @@ __device__ inline void drop_row(const LArgs &a, int b, int segment) {
     // no cut inside a page that others hold, none behind what the window has left
     const int at = keep >> r.page_shift;
     const int id = (keep & ((1 << r.page_shift) - 1)) && at < r.max_pages ? row[at] : -1;
-    refused = in_pool(id, r.n_pages) && read_now(&a.holders[id]) > 1;
+    refused = in_pool(id, r.n_pages) && a.holders[id] > 1;
     if (x.gone > 0 && (W == 0 || keep - W + 1 < x.gone)) refused = true;
   }
   if (refused) keep = x.L;
@@ -212,69 +215,71 @@ __device__ inline void drop_row(const LArgs &a, int b, int segment) {
   }
   const Held h = held(r, x.L, x.gone);
   const Held after = held(r, keep, gone);
-  const int i1 = min((segment + 1) * kSegment, h.count());
-  for (int i = segment * kSegment + lane; i < i1; i += 64) {
-    const int j = h.entry(i), id = after.has(j) ? -1 : row[j];
-    if (!in_pool(id, r.n_pages)) continue;
-    if (atomicAdd(&a.dropped[id], 1) + 1 == read_now(&a.holders[id])) atomicAdd(&a.freed[id / kChunk], 1);
+  const int n = h.count(), i0 = segment * kSegment + lane;
+  int id[kPer], mine[kPer], before[kPer];
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int j = i0 + u * 64 < n ? h.entry(i0 + u * 64) : -1;
+    id[u] = j < 0 || after.has(j) ? -1 : row[j];
   }
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    mine[u] = in_pool(id[u], r.n_pages) ? a.holders[id[u]] : 0;
+    before[u] = in_pool(id[u], r.n_pages) ? atomicAdd(&a.dropped[id[u]], 1) : 0;
+  }
+#pragma unroll
+  for (int u = 0; u < kPer; ++u)
+    if (mine[u] > 0 && before[u] + 1 == mine[u]) atomicAdd(&a.freed[id[u] / kChunk], 1);
 }
 
-// THREADS threads push the freed pages [p0, p0 + kChunk) from place `at` on.
-template <int THREADS>
-__device__ inline int push_chunk(const LArgs &a, int p0, int at, int *wsum) {
-  constexpr int PER = kChunk / THREADS, WAVES = THREADS / 64;
-  const int tid = threadIdx.x, wave = tid >> 6;
-  uint32_t mine = 0;
-#pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int p = p0 + tid * PER + i;
-    if (p >= a.r.n_pages) break;
-    const int n = read_now(&a.holders[p]);
-    mine |= (n > 0 && read_now(&a.dropped[p]) == n ? 1u : 0u) << i;
-  }
-  const int n = __builtin_popcount(mine);
+__device__ inline int stack_of(const PageRelease &r) { return min(max(0, r.free_count[0]), r.n_pages); }
+
+// the counts, which lie in one piece
+__global__ __launch_bounds__(kThreads) void page_release_clear_kernel(int4 *ws, long long n) {
+  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
+  if (i < n) ws[i] = make_int4(0, 0, 0, 0);
+}
+// a wave for each segment of a row
+__device__ inline int row_segment(const LArgs &a, int &segment) {
+  const unsigned w = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  segment = (int)(w % (unsigned)a.segments);
+  return (int)(w / (unsigned)a.segments);
+}
+__global__ __launch_bounds__(kThreads) void page_release_count_kernel(LArgs a) {
+  int segment;
+  const int b = row_segment(a, segment);
+  if (b < a.r.B) count_row(a, b, segment);
+}
+__global__ __launch_bounds__(kThreads) void page_release_drop_kernel(LArgs a) {
+  int segment;
+  const int b = row_segment(a, segment);
+  if (b < a.r.B) drop_row(a, b, segment);
+}
+// Block i pushes the freed ones of the pages [1024 i, 1024 (i + 1)), four a thread.
+__global__ __launch_bounds__(kThreads) void page_release_push_kernel(LArgs a) {
+  __shared__ int wsum[kWaves];
+  const int tid = threadIdx.x, wave = tid >> 6, p0 = blockIdx.x * kChunk + tid * 4;
+  const int4 h = *reinterpret_cast<const int4 *>(a.holders + p0), d = *reinterpret_cast<const int4 *>(a.dropped + p0);
+  int sum = 0;
+  for (int i = tid; i < (int)blockIdx.x; i += kThreads) sum += a.freed[i];
+  int at = stack_of(a.r) + block_sum<kWaves>(sum, wsum);
+  const bool f[4] = {h.x > 0 && h.x == d.x, h.y > 0 && h.y == d.y, h.z > 0 && h.z == d.z, h.w > 0 && h.w == d.w};
+  const int n = f[0] + f[1] + f[2] + f[3];
   const int incl = (int)wave::prefix_sum((uint32_t)n);
   __syncthreads();
   if ((tid & 63) == 63) wsum[wave] = incl;
   __syncthreads();
-  int total = 0;
 #pragma unroll
-  for (int w = 0; w < WAVES; ++w) {
+  for (int w = 0; w < kWaves; ++w)
     if (w < wave) at += wsum[w];
-    total += wsum[w];
-  }
   at += incl - n;
 #pragma unroll
-  for (int i = 0; i < PER; ++i)
-    if (mine >> i & 1) {
-      if (at < a.r.n_pages) a.r.free_pages[at] = p0 + tid * PER + i;
+  for (int i = 0; i < 4; ++i)
+    if (f[i]) {
+      if (at < a.r.n_pages) a.r.free_pages[at] = p0 + i;
       ++at;
     }
-  return total;
-}
-__device__ inline int stack_of(const PageRelease &r) { return min(max(0, r.free_count[0]), r.n_pages); }
-
-// holders, dropped and freed lie in one piece
-__global__ __launch_bounds__(kThreads) void page_release_clear_kernel(int *ws, long long n) {
-  const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
-  if (i < n) ws[i] = 0;
-}
-__global__ __launch_bounds__(kThreads) void page_release_count_kernel(LArgs a) {
-  const int w = blockIdx.x * kWaves + (threadIdx.x >> 6), b = w / a.segments;
-  if (b < a.r.B) count_row(a, b, w % a.segments);
-}
-__global__ __launch_bounds__(kThreads) void page_release_drop_kernel(LArgs a) {
-  const int w = blockIdx.x * kWaves + (threadIdx.x >> 6), b = w / a.segments;
-  if (b < a.r.B) drop_row(a, b, w % a.segments);
-}
-__global__ __launch_bounds__(kThreads) void page_release_push_kernel(LArgs a) {
-  __shared__ int wsum[kWaves];
-  int sum = 0;
-  for (int i = threadIdx.x; i < (int)blockIdx.x; i += kThreads) sum += a.freed[i];
-  const int at = stack_of(a.r) + block_sum<kWaves>(sum, wsum);
-  const int n = push_chunk<kThreads>(a, blockIdx.x * kChunk, at, wsum);
-  if (blockIdx.x == gridDim.x - 1 && threadIdx.x == 0) a.r.free_count_out[0] = min(at + n, a.r.n_pages);
+  if (blockIdx.x == gridDim.x - 1 && tid == kThreads - 1) a.r.free_count_out[0] = min(at, a.r.n_pages);
 }
 
 }  // namespace
@@ -299,7 +304,7 @@ hipError_t launch_page_copy(hipStream_t st, const avtp_pages &P, const int32_t *
   a.src = src_page;
   a.dst = dst_page;
   a.page_bytes = (long long)P.Hkv * P.page_size * P.d * (P.dtype == AVTP_FP32 ? 4 : 2);
-  constexpr int kBytes = kThreads * kUnits * 16;
+  constexpr int kBytes = kThreads * 16;
   a.chunks = (int)((a.page_bytes + kBytes - 1) / kBytes);
   a.n_pages = P.n_pages;
   // (blocks of 256 threads, fewer than 2^24 in a launch)
@@ -315,27 +320,26 @@ hipError_t launch_page_copy(hipStream_t st, const avtp_pages &P, const int32_t *
   return hipSuccess;
 }
 
-size_t page_release_workspace_bytes(int n_pages) {
-  return 4 * (2 * (size_t)n_pages + ((size_t)n_pages + kChunk - 1) / kChunk);
-}
+// holders and dropped, whole chunks of them, and freed
+static size_t chunks_of(int n_pages) { return ((size_t)n_pages + kChunk - 1) / kChunk; }
+size_t page_release_workspace_bytes(int n_pages) { return (2 * kChunk * 4 + 4) * chunks_of(n_pages) + 12; }
 
 hipError_t launch_page_release(hipStream_t st, const PageRelease &R, int32_t *ws) {
   clear_pending_error();
   LArgs a;
   a.r = R;
+  const size_t chunks = chunks_of(R.n_pages);
   a.holders = ws;
-  a.dropped = ws + R.n_pages;
-  a.freed = ws + 2 * (size_t)R.n_pages;
+  a.dropped = ws + chunks * kChunk;
+  a.freed = ws + 2 * chunks * kChunk;
   a.segments = (R.max_pages + kSegment - 1) / kSegment;
-  const long long words = (long long)page_release_workspace_bytes(R.n_pages) / 4;
-  const long long waves = (long long)R.B * a.segments;
+  const long long units = (long long)((2 * chunks * kChunk + chunks + 3) / 4), waves = (long long)R.B * a.segments;
   const dim3 rows((unsigned)((waves + kWaves - 1) / kWaves));
-  hipLaunchKernelGGL(page_release_clear_kernel, dim3((unsigned)((words + kThreads - 1) / kThreads)), dim3(kThreads), 0,
-                     st, ws, words);
+  hipLaunchKernelGGL(page_release_clear_kernel, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), 0,
+                     st, (int4 *)ws, units);
   hipLaunchKernelGGL(page_release_count_kernel, rows, dim3(kThreads), 0, st, a);
   hipLaunchKernelGGL(page_release_drop_kernel, rows, dim3(kThreads), 0, st, a);
-  hipLaunchKernelGGL(page_release_push_kernel, dim3((unsigned)((R.n_pages + kChunk - 1) / kChunk)), dim3(kThreads), 0,
-                     st, a);
+  hipLaunchKernelGGL(page_release_push_kernel, dim3((unsigned)chunks), dim3(kThreads), 0, st, a);
   return hipGetLastError();
 }
 

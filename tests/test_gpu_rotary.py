@@ -221,6 +221,18 @@ def test_stream_and_graph():
         assert torch.equal(q, eager)
 
 
+@pytest.mark.parametrize("dtype, n", [(BF, 17001), (F, 8501)])
+def test_large_outputs_past_the_caches(dtype, n):
+    x = Rows(13, dtype, n, 32, 8, 128, 3)
+    rotary = Rotary(128, base=1e6, planes=[i % 3 for i in range(64)])
+    q, k = A.norm_rotary(rotary, x.pos, x.q, x.k, x.wq, x.wk)
+    for r in (slice(0, n // 2), slice(n // 2, n)):       # each half below the border
+        a, b = A.norm_rotary(rotary, x.pos[:, r], x.q[r], x.k[r], x.wq, x.wk)
+        assert torch.equal(q[r], a) and torch.equal(k[r], b)
+    some = torch.tensor([0, n // 2, n - 1], device="cuda")
+    check(q[some], oracle(rotary, x.q[some], x.pos[:, some], x.wq, 1e-6), dtype, "q")
+
+
 def test_nothing_to_do():
     rotary = Rotary(64)
     e = torch.empty(0, 2, 64, dtype=BF, device="cuda")
