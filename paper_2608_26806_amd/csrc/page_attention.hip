@@ -500,18 +500,23 @@ __device__ __attribute__((always_inline)) inline void attend(const A &a, const J
   // Values of V that are not finite, in a tile that some row sees only in
   // part: 0 times them is not 0.  The tile's product then runs without them
   // and they are added to the rows that see them.
-  auto not_finite = [&](uint32_t x) __attribute__((always_inline)) {
-    return F32 ? (x & 0x7f800000u) == 0x7f800000u : ((((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0u);
-  };
+  // (In fp32 they are found in a sum of 0 times the values, one instruction each: one
+  // prompt of 1,000 tokens, 16/8 heads of 128, window 512 67.5 -> 65.7 us; in bf16 sums
+  // of squares gained nothing over the integer test.)
   auto tile_not_finite = [&](lptr vt) __attribute__((always_inline)) {
     bool bad = false;
+    float sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kTile * NCH / 64; ++i) {
       const u32x4 x = *reinterpret_cast<AVTP_LDS const u32x4 *>(vt + (i * 64 + lane) * 16);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) bad = bad || not_finite(x[j]);
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t u = x[j];  // (an element cast in place is read as the vector's first)
+        if constexpr (F32) sum = __builtin_fmaf(__builtin_bit_cast(float, u), 0.f, sum);
+        else bad = bad || (((u & 0x7f807f80u) + 0x00800080u) & 0x80008000u) != 0u;
+      }
     }
-    return __ballot(bad) != 0ull;
+    return __ballot(F32 ? sum != 0.f : bad) != 0ull;  // (a sum of NaN)
   };
   auto add_not_finite = [&](lptr vt, int key) __attribute__((always_inline)) {
 #pragma unroll 1
@@ -1090,6 +1095,8 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   const int64_t brief = tiles_of(small);
   L.brief = P.dtype == AVTP_BF16 && brief <= (P.d == 64 ? kShortTiles64 : kShortTiles) &&
             max_kv_len <= (small == 32 && brief >= kShortFull ? kShortFullKeys : kShortKeys);
+  // (the tiles of sequences of equally many rows)
+  const int64_t now = ((rows + small - 1) / small > B ? (rows + small - 1) / small : B) * P.Hkv;
   // Behind a window most sequences see equally much (told by a bound of twice the window
   // or more), so that blocks of single tokens end together: four waves or two a tile, where
   // they are on half of the CUs in one round or fill 0.7 of the places of several.  One
@@ -1100,7 +1107,6 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // 25.6 (four 30.9); window 3,000, 8 26.6 / 35.9, 40 86.6 / 88.4, 80 (two 0.63 full) 164 /
   // 181, 96 194 / 182; 16/16 heads of 64, window 1,024, 8 (128 tiles) 17.5 / 14.1.
   if (alike && !L.brief && P.dtype == AVTP_BF16 && small == 16) {
-    const int64_t now = ((rows + 15) / 16 > B ? (rows + 15) / 16 : B) * P.Hkv;
     // the part of their places that the blocks of the last round and those before fill
     auto fill = [&](int waves) {
       const int64_t places = 1024 / waves * (P.d == 64 ? 2 : 1), rounds = (now + places - 1) / places;
@@ -1112,6 +1118,17 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     L.half = !(four > 0 && (once || (max_kv_len > 512 && four > 1.12 * two)));
     L.brief = four > 0 || two > 0;
     if (L.half && two == 0.) L.brief = false;
+  }
+  // fp32 behind a window: where a block's waves (four, or two at d 128) have a few stages
+  // each.  us, line or blocks of 128 rows against blocks that join, d 64 (14/2 heads) and
+  // d 128 (16/8): 100 tokens, window 64 17.0 / 8.4 and 26.5 / 17.3, 256 18.9 / 14.2 and 27.6
+  // / 32.6, 1,000 21.0 / 30.0; 300 tokens (131 tiles), 1,000 42.8 / 30.9; 1,000 tokens (440
+  // tiles), 256 31.9 / 28.3, 1,000 57.8 / 60.1; one token, 64 11.0 / 5.5 and 15.0 / 10.4, 256
+  // 11.3 / 9.0 and 15.2 / 18.5; 32 requests, 256 11.0 / 13.3 and (256 tiles) 32.1 / 27.2.
+  if (w.window > 0 && P.dtype == AVTP_FP32) {
+    const bool full = now >= kShortFull, narrow = P.d == 64;
+    const int64_t most = narrow && small == 32 ? (full ? kShortFullKeys : 512) : !narrow && small == 16 && full && alike ? seen : 128;
+    L.brief = now <= 256 ? max_kv_len <= most : narrow && small == 32 && now <= 512 && max_kv_len <= 260;
   }
   // Up to 32 rows a sequence is one tile of the even line; more rows read its keys once
   // per 32 there and once per 128 in a block.  us, line against blocks: 28/4 heads, 64
@@ -1182,13 +1199,14 @@ template <typename T, int D, typename A>
 static hipError_t launch(hipStream_t st, const PageAttnPlan &L, const A &k) {
   constexpr int TPW = many_tiles(D * (int)sizeof(T));
   const dim3 grid((unsigned)L.blocks);
-  if constexpr (sizeof(T) == 2) {
+  if constexpr (sizeof(T) == 2 || A::WIN) {
     if (L.brief) {
       auto run = [&](auto m_tag, auto w_tag) {
         constexpr int M = decltype(m_tag)::value, W = decltype(w_tag)::value;
         hipLaunchKernelGGL((page_attn_short_kernel<T, D, M, W, A>), grid, dim3(64 * W), 0, st, k);
       };
-      constexpr std::integral_constant<int, kShortWaves> all{};
+      // (fp32 rows of 512 bytes: two waves' buffers fill the LDS)
+      constexpr std::integral_constant<int, kShortWaves * (D * (int)sizeof(T) > 256 ? 2 : 4) / 4> all{};
       if (L.tile == 32) run(std::integral_constant<int, 32>{}, all);
       else if (!A::WIN || !L.half) run(std::integral_constant<int, 16>{}, all);
       else if constexpr (A::WIN) run(std::integral_constant<int, 16>{}, std::integral_constant<int, kShortWaves / 2>{});

@@ -138,6 +138,20 @@ def test_more_than_64_sequences():
         assert not c.status.any()
 
 
+@pytest.mark.parametrize("dtype, Hq, Hkv, d, B", [(BF, 8, 8, 128, 70), (BF, 14, 2, 128, 230), (BF, 8, 8, 64, 150),
+                                                  (BF, 16, 8, 64, 80), (F, 8, 8, 128, 20), (F, 4, 4, 64, 50)])
+def test_many_single_tokens_behind_a_window(dtype, Hq, Hkv, d, B):
+    # blocks of two waves and of four, one round and several; some sequences are short
+    rng = np.random.default_rng(B)
+    kv = rng.integers(1, 700, B)
+    for window, sinks in ((40, 4), (150, 0)):
+        c = Case(B, dtype, Hq, Hkv, d, 16, [1] * B, kv.tolist(), window, sinks)
+        ref = c.oracle()
+        c.check(c.run(), ref)
+        c.check(c.run(max_kv=100000), ref)
+        assert not c.status.any()
+
+
 @pytest.mark.parametrize("dtype", [BF, F])
 @pytest.mark.parametrize("new, kv", [([1] * 5, [700, 300, 40, 1, 129]), ([50, 1, 200], [600, 500, 900])])
 def test_pages_that_left_the_window_are_not_looked_at(dtype, new, kv):
