@@ -774,10 +774,41 @@ __device__ __attribute__((always_inline)) inline void attend(const A &a, const J
   }
   l = over_row<M>(l, [](float x, float y) { return x + y; });
 
-  // the finished rows, or the tile's part
-  if (!valid) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   const float ls = l == 0.f ? -INFINITY : m + __builtin_amdgcn_logf(l);  // log2 of the row's sum
+  if constexpr (WIN && WR > 1 && !F32) {
+    if (!job.cut) {
+      // Finished rows of 128 tokens and heads, whose stores weigh more the shorter the
+      // window: turned around in LDS, 16 bytes a lane and a row in one piece (four prompts
+      // of 7,000-9,000 tokens, 32/8 heads, window 64 251 -> 196 us, 512 442 -> 433, 2,048
+      // 1056 -> 1047).  The other stage buffer is free: all waves passed the last stage's
+      // barrier, and nothing is on its way to it.
+      AVTP_LDS char *const mine = bufB + wave * M * ROWB;
+      auto at = [&](int r, int ch) __attribute__((always_inline)) { return mine + r * ROWB + ((ch ^ (r & (NCH - 1))) << 4); };
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+        for (int j = 0; j < AE / 4; ++j) {
+          const int dd = M * dt + eoff(4 * j) + 4 * grp;
+          bf16x4 y;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) y[i] = (__bf16)(O[dt][4 * j + i] * inv);
+          *reinterpret_cast<AVTP_LDS bf16x4 *>(at(col, dd / 8) + (dd & 4) * 2) = y;
+        }
+#pragma unroll
+      for (int i = 0; i < M * NCH / 64; ++i) {
+        const int r = i * RPL + lane / NCH, ch = lane % NCH, t = (wrow + r) / a.G, h = g * a.G + (wrow + r - t * a.G);
+        const u32x4 x = *reinterpret_cast<AVTP_LDS const u32x4 *>(at(r, ch));
+        if (wrow + r < R)
+          *reinterpret_cast<u32x4 *>(a.out + (job.s.q0 + t) * a.out_tok + (long long)h * ROWB + ch * 16) = x;
+      }
+      if (valid && grp == 0 && a.lse) a.lse[(long long)head * a.N_q + job.s.q0 + tok] = ls * kLn2;
+      return;
+    }
+  }
+
+  // the finished rows, or the tile's part
+  if (!valid) return;
   const long long pr = (long long)job.slot * BM + wave * M + col;
   char *o = a.out + (job.s.q0 + tok) * a.out_tok + (long long)head * ROWB;
 #pragma unroll
