@@ -140,23 +140,21 @@ __global__ __launch_bounds__(kThreads) void page_copy_kernel(CArgs a) {
 // pages of the sinks.  A page goes back when all rows that held it before the call
 // let it go: `holders` counts the rows before, `dropped` those that let go, both
 // by integer atomics, whose order does not show.  Freed pages are pushed by number.
-// `freed` counts them by chunks of pages, so that every block of the last launch
-// knows its place.
+//
+// Small pools are counted in the LDS of one block, in one launch: 64 requests that
+// share eight prompts (15,000 entries) take 8.2 us, two requests 3.5; in four launches
+// over the chip, which count in a workspace (clear, count, drop, push), 14.6 and 14.5,
+// mostly the launches.  128 requests of 100 entries 8.3 against 15.0 (256 of them 16 us
+// in a block of 1,024 rows).  1,024 requests behind a window, 68,000 entries: 16.3.
 
-struct LArgs {
-  PageRelease r;
-  int *holders, *dropped, *freed;  // workspace
-  int segments;                    // of a row, kSegment entries each
-};
-constexpr int kPer = 4;                  // entries of a row per lane, their loads in flight together
-constexpr int kSegment = 64 * kPer;      // and of a wave
-constexpr int kChunk = kThreads * 4;     // pages whose freed ones are counted together
+constexpr int kPer = 4;               // entries of a row per lane
+constexpr int kSegment = 64 * kPer;   // and of a wave
+constexpr int kChunk = kThreads * 4;  // pages whose freed ones are counted together
 
 struct Held {
   int end, sinks, first;  // pages of the row: [0, sinks) and [first, end)
   __device__ inline int count() const { return sinks + max(0, end - first); }
   __device__ inline int entry(int i) const { return i < sinks ? i : first + i - sinks; }
-  __device__ inline bool has(int j) const { return j < sinks || (j >= first && j < end); }
 };
 __device__ inline Held held(const PageRelease &r, int tokens, int gone) {
   Held h;
@@ -166,74 +164,157 @@ __device__ inline Held held(const PageRelease &r, int tokens, int gone) {
   h.first = max(s, gone >> r.page_shift);
   return h;
 }
+// what `before` holds and `after` does not: up to three runs of a row
+struct Gone {
+  int a0, a1, b0, b1, c0, c1;
+  __device__ inline Gone(const Held &before, const Held &after)
+      : a0(after.sinks), a1(before.sinks), b0(before.first), b1(max(b0, min(after.first, before.end))),
+        c0(max(b1, after.end)), c1(before.end) {}
+  __device__ inline int count() const { return max(0, a1 - a0) + (b1 - b0) + max(0, c1 - c0); }
+  __device__ inline int entry(int i) const {
+    const int a = max(0, a1 - a0);
+    if (i < a) return a0 + i;
+    return i - a < b1 - b0 ? b0 + i - a : c0 + i - a - (b1 - b0);
+  }
+};
 struct Row {
-  int L, gone;
+  int L, gone, keep;  // before; keep: the tokens asked for, or kept
 };
 __device__ inline Row row_of(const PageRelease &r, int b) {
-  return {max(0, r.seq_len[b]), r.gone ? max(0, r.gone[b]) : 0};
+  const int L = max(0, r.seq_len[b]);
+  return {L, r.gone ? max(0, r.gone[b]) : 0, min(max(0, r.keep_len[b]), L)};
 }
-
-__device__ inline void count_row(const LArgs &a, int b, int segment) {
-  const Row x = row_of(a.r, b);
-  const Held h = held(a.r, x.L, x.gone);
-  const int32_t *row = a.r.table + (size_t)b * a.r.max_pages;
-  const int n = h.count(), i0 = segment * kSegment + (threadIdx.x & 63);
-  int id[kPer];
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) id[u] = i0 + u * 64 < n ? row[h.entry(i0 + u * 64)] : 0;
-  bool bad = false;
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    if (i0 + u * 64 >= n) break;
-    if (in_pool(id[u], a.r.n_pages)) atomicAdd(&a.holders[id[u]], 1);
-    else bad = true;
-  }
-  if (bad && a.r.status) atomicOr(&a.r.status[b], AVTP_FLAG_BAD_PAGE);
-}
-
-__device__ inline void drop_row(const LArgs &a, int b, int segment) {
-  const PageRelease &r = a.r;
-  const int lane = threadIdx.x & 63, W = r.window;
-  const Row x = row_of(r, b);
-  const int32_t *row = r.table + (size_t)b * r.max_pages;
-  int keep = min(max(0, r.keep_len[b]), x.L), gone = x.gone;
+// What row b keeps, and of its window; with `say` it is written down.
+__device__ inline Row kept(const PageRelease &r, int b, const Row &x, const int *holders, bool say) {
+  const int W = r.window;
+  Row y = x;
   bool refused = false;
-  if (keep > 0 && keep < x.L) {
+  if (x.keep > 0 && x.keep < x.L) {
     // no cut inside a page that others hold, none behind what the window has left
-    const int at = keep >> r.page_shift;
-    const int id = (keep & ((1 << r.page_shift) - 1)) && at < r.max_pages ? row[at] : -1;
-    refused = in_pool(id, r.n_pages) && a.holders[id] > 1;
-    if (x.gone > 0 && (W == 0 || keep - W + 1 < x.gone)) refused = true;
+    const int at = x.keep >> r.page_shift;
+    const bool inside = (x.keep & ((1 << r.page_shift) - 1)) && at < r.max_pages;
+    const int id = inside ? r.table[(size_t)b * r.max_pages + at] : -1;
+    refused = in_pool(id, r.n_pages) && holders[id] > 1;
+    if (x.gone > 0 && (W == 0 || x.keep - W + 1 < x.gone)) refused = true;
   }
-  if (refused) keep = x.L;
-  else if (keep == 0) gone = 0;
-  else if (W > 0) gone = max(gone, keep - W + 1);
-  if (segment == 0 && lane == 0) {
-    r.seq_len_out[b] = keep;
-    if (r.gone_out) r.gone_out[b] = gone;
+  if (refused) y.keep = x.L;
+  else if (x.keep == 0) y.gone = 0;
+  else if (W > 0) y.gone = max(x.gone, x.keep - W + 1);
+  if (say) {
+    r.seq_len_out[b] = y.keep;
+    if (r.gone_out) r.gone_out[b] = y.gone;
     if (refused && r.status) atomicOr(&r.status[b], AVTP_FLAG_REFUSED);
   }
-  const Held h = held(r, x.L, x.gone);
-  const Held after = held(r, keep, gone);
-  const int n = h.count(), i0 = segment * kSegment + lane;
-  int id[kPer], mine[kPer], before[kPer];
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    const int j = i0 + u * 64 < n ? h.entry(i0 + u * 64) : -1;
-    id[u] = j < 0 || after.has(j) ? -1 : row[j];
-  }
-#pragma unroll
-  for (int u = 0; u < kPer; ++u) {
-    mine[u] = in_pool(id[u], r.n_pages) ? a.holders[id[u]] : 0;
-    before[u] = in_pool(id[u], r.n_pages) ? atomicAdd(&a.dropped[id[u]], 1) : 0;
-  }
-#pragma unroll
-  for (int u = 0; u < kPer; ++u)
-    if (mine[u] > 0 && before[u] + 1 == mine[u]) atomicAdd(&a.freed[id[u] / kChunk], 1);
+  return y;
 }
 
+// LANES lanes count the entries i0 .. of what row b holds, PER each, their loads in
+// flight together.
+template <int LANES, int PER>
+__device__ inline void count_entries(const PageRelease &r, int b, const Held &h, int i0, int *holders) {
+  const int32_t *row = r.table + (size_t)b * r.max_pages;
+  const int n = h.count(), i = i0 + (int)(threadIdx.x % LANES);
+  int id[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) id[u] = i + u * LANES < n ? row[h.entry(i + u * LANES)] : 0;
+  bool bad = false;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) {
+    if (i + u * LANES >= n) break;
+    if (in_pool(id[u], r.n_pages)) atomicAdd(&holders[id[u]], 1);
+    else bad = true;
+  }
+  if (bad && r.status) atomicOr(&r.status[b], AVTP_FLAG_BAD_PAGE);
+}
+// And let go of the entries i0 .. of what it holds no longer; freed: by chunks, or null.
+template <int LANES, int PER>
+__device__ inline void drop_entries(const PageRelease &r, int b, const Gone &g, int i0, const int *holders,
+                                    int *dropped, int *freed) {
+  const int32_t *row = r.table + (size_t)b * r.max_pages;
+  const int n = g.count(), i = i0 + (int)(threadIdx.x % LANES);
+  int id[PER], before[PER];
+#pragma unroll
+  for (int u = 0; u < PER; ++u) id[u] = i + u * LANES < n ? row[g.entry(i + u * LANES)] : -1;
+#pragma unroll
+  for (int u = 0; u < PER; ++u) before[u] = in_pool(id[u], r.n_pages) ? atomicAdd(&dropped[id[u]], 1) : 0;
+  if (!freed) return;
+#pragma unroll
+  for (int u = 0; u < PER; ++u)
+    if (in_pool(id[u], r.n_pages) && before[u] + 1 == holders[id[u]]) atomicAdd(&freed[id[u] / kChunk], 1);
+}
 __device__ inline int stack_of(const PageRelease &r) { return min(max(0, r.free_count[0]), r.n_pages); }
 
+// Four pages from p0 on for each of the block's threads: the freed ones go onto the
+// stack from place `at` on, which moves up.
+template <int WAVES>
+__device__ inline void push_freed(const PageRelease &r, int p0, const int4 &h, const int4 &d, int &at, int *wsum) {
+  const int tid = threadIdx.x, wave = tid >> 6;
+  const bool f[4] = {h.x > 0 && h.x == d.x, h.y > 0 && h.y == d.y, h.z > 0 && h.z == d.z, h.w > 0 && h.w == d.w};
+  const int n = f[0] + f[1] + f[2] + f[3];
+  const int incl = (int)wave::prefix_sum((uint32_t)n);
+  __syncthreads();  // wsum's last readers are done
+  if ((tid & 63) == 63) wsum[wave] = incl;
+  __syncthreads();
+  int place = at + incl - n;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    if (w < wave) place += wsum[w];
+    at += wsum[w];
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (f[i]) {
+      if (place < r.n_pages) r.free_pages[place] = p0 + i;
+      ++place;
+    }
+}
+
+constexpr int kSmallThreads = 1024, kSmallWaves = kSmallThreads / 64;
+constexpr int kSmallRows = 128;
+constexpr long long kSmallEntries = 1 << 17;  // of the table, of which few rows fill theirs
+constexpr int kSmallPages = 16384;           // whose counts fill 128 KB of LDS
+constexpr int kGroup = 32;                   // lanes that walk a row, kPer entries each at a time
+__global__ __launch_bounds__(kSmallThreads) void page_release_small_kernel(PageRelease r) {
+  __shared__ __attribute__((aligned(16))) int holders[kSmallPages], dropped[kSmallPages];
+  __shared__ Row before[kSmallRows], after[kSmallRows];
+  __shared__ int wsum[kSmallWaves];
+  const int tid = threadIdx.x;
+  int at = stack_of(r);
+  if (tid < r.B) before[tid] = row_of(r, tid);
+  for (int i = tid * 4; i < r.n_pages; i += kSmallThreads * 4)
+    *reinterpret_cast<int4 *>(holders + i) = *reinterpret_cast<int4 *>(dropped + i) = make_int4(0, 0, 0, 0);
+  __syncthreads();
+  constexpr int kGroups = kSmallThreads / kGroup;
+  for (int b = tid / kGroup; b < r.B; b += kGroups) {
+    const Held h = held(r, before[b].L, before[b].gone);
+    for (int i0 = 0; i0 < h.count(); i0 += kGroup * kPer) count_entries<kGroup, kPer>(r, b, h, i0, holders);
+  }
+  __syncthreads();
+  if (tid < r.B) after[tid] = kept(r, tid, before[tid], holders, true);
+  __syncthreads();
+  for (int b = tid / kGroup; b < r.B; b += kGroups) {
+    const Gone g(held(r, before[b].L, before[b].gone), held(r, after[b].keep, after[b].gone));
+    for (int i0 = 0; i0 < g.count(); i0 += kGroup * kPer)
+      drop_entries<kGroup, kPer>(r, b, g, i0, holders, dropped, nullptr);
+  }
+  __syncthreads();
+  for (int p0 = 0; p0 < r.n_pages; p0 += kSmallThreads * 4) {
+    const int p = p0 + tid * 4;
+    int4 h = make_int4(0, 0, 0, 0), d = h;
+    if (p < r.n_pages) {
+      h = *reinterpret_cast<const int4 *>(holders + p);
+      d = *reinterpret_cast<const int4 *>(dropped + p);
+    }
+    push_freed<kSmallWaves>(r, p, h, d, at, wsum);
+  }
+  if (tid == 0) r.free_count_out[0] = min(at, r.n_pages);
+}
+
+struct LArgs {
+  PageRelease r;
+  int *holders, *dropped, *freed;  // workspace
+  int segments;                    // of a row, kSegment entries each
+};
 // the counts, which lie in one piece
 __global__ __launch_bounds__(kThreads) void page_release_clear_kernel(int4 *ws, long long n) {
   const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
@@ -248,38 +329,28 @@ __device__ inline int row_segment(const LArgs &a, int &segment) {
 __global__ __launch_bounds__(kThreads) void page_release_count_kernel(LArgs a) {
   int segment;
   const int b = row_segment(a, segment);
-  if (b < a.r.B) count_row(a, b, segment);
+  if (b >= a.r.B) return;
+  const Row x = row_of(a.r, b);
+  count_entries<64, kPer>(a.r, b, held(a.r, x.L, x.gone), segment * kSegment, a.holders);
 }
 __global__ __launch_bounds__(kThreads) void page_release_drop_kernel(LArgs a) {
   int segment;
   const int b = row_segment(a, segment);
-  if (b < a.r.B) drop_row(a, b, segment);
+  if (b >= a.r.B) return;
+  const Row x = row_of(a.r, b), y = kept(a.r, b, x, a.holders, segment == 0 && (threadIdx.x & 63) == 0);
+  const Gone g(held(a.r, x.L, x.gone), held(a.r, y.keep, y.gone));
+  drop_entries<64, kPer>(a.r, b, g, segment * kSegment, a.holders, a.dropped, a.freed);
 }
 // Block i pushes the freed ones of the pages [1024 i, 1024 (i + 1)), four a thread.
 __global__ __launch_bounds__(kThreads) void page_release_push_kernel(LArgs a) {
   __shared__ int wsum[kWaves];
-  const int tid = threadIdx.x, wave = tid >> 6, p0 = blockIdx.x * kChunk + tid * 4;
+  const int tid = threadIdx.x, p0 = blockIdx.x * kChunk + tid * 4;
   const int4 h = *reinterpret_cast<const int4 *>(a.holders + p0), d = *reinterpret_cast<const int4 *>(a.dropped + p0);
   int sum = 0;
   for (int i = tid; i < (int)blockIdx.x; i += kThreads) sum += a.freed[i];
   int at = stack_of(a.r) + block_sum<kWaves>(sum, wsum);
-  const bool f[4] = {h.x > 0 && h.x == d.x, h.y > 0 && h.y == d.y, h.z > 0 && h.z == d.z, h.w > 0 && h.w == d.w};
-  const int n = f[0] + f[1] + f[2] + f[3];
-  const int incl = (int)wave::prefix_sum((uint32_t)n);
-  __syncthreads();
-  if ((tid & 63) == 63) wsum[wave] = incl;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w)
-    if (w < wave) at += wsum[w];
-  at += incl - n;
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (f[i]) {
-      if (at < a.r.n_pages) a.r.free_pages[at] = p0 + i;
-      ++at;
-    }
-  if (blockIdx.x == gridDim.x - 1 && tid == kThreads - 1) a.r.free_count_out[0] = min(at, a.r.n_pages);
+  push_freed<kWaves>(a.r, p0, h, d, at, wsum);
+  if (blockIdx.x == gridDim.x - 1 && tid == 0) a.r.free_count_out[0] = min(at, a.r.n_pages);
 }
 
 }  // namespace
@@ -333,6 +404,10 @@ hipError_t launch_page_release(hipStream_t st, const PageRelease &R, int32_t *ws
   a.dropped = ws + chunks * kChunk;
   a.freed = ws + 2 * chunks * kChunk;
   a.segments = (R.max_pages + kSegment - 1) / kSegment;
+  if (R.n_pages <= kSmallPages && R.B <= kSmallRows && (long long)R.B * R.max_pages <= kSmallEntries) {
+    hipLaunchKernelGGL(page_release_small_kernel, dim3(1), dim3(kSmallThreads), 0, st, R);
+    return hipGetLastError();
+  }
   const long long units = (long long)((2 * chunks * kChunk + chunks + 3) / 4), waves = (long long)R.B * a.segments;
   const dim3 rows((unsigned)((waves + kWaves - 1) / kWaves));
   hipLaunchKernelGGL(page_release_clear_kernel, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), 0,
