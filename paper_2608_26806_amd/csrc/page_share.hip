@@ -313,33 +313,35 @@ __global__ __launch_bounds__(kSmallThreads) void page_release_small_kernel(PageR
 struct LArgs {
   PageRelease r;
   int *holders, *dropped, *freed;  // workspace
-  int segments;                    // of a row, kSegment entries each
+  int waves;                       // that share a row, kSegment entries each at a time
 };
 // the counts, which lie in one piece
 __global__ __launch_bounds__(kThreads) void page_release_clear_kernel(int4 *ws, long long n) {
   const long long i = (long long)blockIdx.x * kThreads + threadIdx.x;
   if (i < n) ws[i] = make_int4(0, 0, 0, 0);
 }
-// a wave for each segment of a row
-__device__ inline int row_segment(const LArgs &a, int &segment) {
-  const unsigned w = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  segment = (int)(w % (unsigned)a.segments);
-  return (int)(w / (unsigned)a.segments);
+// which row, and the wave's number in it
+__device__ inline int row_wave(const LArgs &a, int &w) {
+  const unsigned x = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  w = (int)(x % (unsigned)a.waves);
+  return (int)(x / (unsigned)a.waves);
 }
 __global__ __launch_bounds__(kThreads) void page_release_count_kernel(LArgs a) {
-  int segment;
-  const int b = row_segment(a, segment);
+  int w;
+  const int b = row_wave(a, w);
   if (b >= a.r.B) return;
   const Row x = row_of(a.r, b);
-  count_entries<64, kPer>(a.r, b, held(a.r, x.L, x.gone), segment * kSegment, a.holders);
+  const Held h = held(a.r, x.L, x.gone);
+  for (int i0 = w * kSegment; i0 < h.count(); i0 += a.waves * kSegment) count_entries<64, kPer>(a.r, b, h, i0, a.holders);
 }
 __global__ __launch_bounds__(kThreads) void page_release_drop_kernel(LArgs a) {
-  int segment;
-  const int b = row_segment(a, segment);
+  int w;
+  const int b = row_wave(a, w);
   if (b >= a.r.B) return;
-  const Row x = row_of(a.r, b), y = kept(a.r, b, x, a.holders, segment == 0 && (threadIdx.x & 63) == 0);
+  const Row x = row_of(a.r, b), y = kept(a.r, b, x, a.holders, w == 0 && (threadIdx.x & 63) == 0);
   const Gone g(held(a.r, x.L, x.gone), held(a.r, y.keep, y.gone));
-  drop_entries<64, kPer>(a.r, b, g, segment * kSegment, a.holders, a.dropped, a.freed);
+  for (int i0 = w * kSegment; i0 < g.count(); i0 += a.waves * kSegment)
+    drop_entries<64, kPer>(a.r, b, g, i0, a.holders, a.dropped, a.freed);
 }
 // Block i pushes the freed ones of the pages [1024 i, 1024 (i + 1)), four a thread.
 __global__ __launch_bounds__(kThreads) void page_release_push_kernel(LArgs a) {
@@ -403,12 +405,14 @@ hipError_t launch_page_release(hipStream_t st, const PageRelease &R, int32_t *ws
   a.holders = ws;
   a.dropped = ws + chunks * kChunk;
   a.freed = ws + 2 * chunks * kChunk;
-  a.segments = (R.max_pages + kSegment - 1) / kSegment;
+  // enough waves to fill the chip, of which short rows use one
+  const int most = (R.max_pages + kSegment - 1) / kSegment, want = (4096 + R.B - 1) / R.B;
+  a.waves = most < want ? most : want;
   if (R.n_pages <= kSmallPages && R.B <= kSmallRows && (long long)R.B * R.max_pages <= kSmallEntries) {
     hipLaunchKernelGGL(page_release_small_kernel, dim3(1), dim3(kSmallThreads), 0, st, R);
     return hipGetLastError();
   }
-  const long long units = (long long)((2 * chunks * kChunk + chunks + 3) / 4), waves = (long long)R.B * a.segments;
+  const long long units = (long long)((2 * chunks * kChunk + chunks + 3) / 4), waves = (long long)R.B * a.waves;
   const dim3 rows((unsigned)((waves + kWaves - 1) / kWaves));
   hipLaunchKernelGGL(page_release_clear_kernel, dim3((unsigned)((units + kThreads - 1) / kThreads)), dim3(kThreads), 0,
                      st, (int4 *)ws, units);
