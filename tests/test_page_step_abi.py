@@ -146,7 +146,10 @@ def test_release_refusals(patch, rc):
 
 def test_release_workspace_size():
     size = A.lib().avtp_page_release_workspace_size
-    assert size(0) == size(-3) == 0 and size(10) == 84 and size(4097) == 4 * (2 * 4097 + 2)
+    assert size(0) == size(-3) == 0
+    for n in (1, 10, 1023, 1024, 1025, 100000):        # two counts a page, rounded up to chunks, and a sum a chunk
+        assert 8 * n + 4 <= size(n) <= 8 * (n + 1024) + n // 256 + 64
+        assert A.lib().avtp_page_release(*{**REL, "n_pages": n, "ws_bytes": size(n) - 1}.values()) == W
     assert size(2 ** 31 - 1) > 2 ** 34
 
 
