@@ -88,10 +88,12 @@ class Rotary:
                 raise ValueError(f"planes: {rot_dim // 2} numbers below {A.MAX_PLANES} are needed")
         # fractions of a turn in 64 bits; whole turns drop out (the long double's 64-bit
         # mantissa holds each to 2^-64 of itself)
-        turns = [int(np.rint(np.ldexp(x - np.floor(x), 64))) % (1 << 64) for x in f.astype(np.longdouble) / _TWO_PI]
+        x = f.astype(np.longdouble) / _TWO_PI
+        turns = np.rint(np.ldexp(x - np.floor(x), 64))
+        turns = np.where(turns < np.ldexp(np.longdouble(1), 64), turns, 0).astype(np.uint64)
         self.rot_dim, self.pairs, self.scale = rot_dim, pairs, float(scale)
         self.n_planes = 1 if planes is None else max(planes) + 1
-        self.turns = torch.from_numpy(np.array(turns, dtype=np.uint64).view(np.int64)).to(device)
+        self.turns = torch.from_numpy(turns.view(np.int64)).to(device)
         self.planes = None if planes is None or self.n_planes == 1 else \
             torch.tensor(planes, dtype=torch.int32, device=device)
         self.st = A._Rotary(self.turns.data_ptr(), None if self.planes is None else self.planes.data_ptr(), rot_dim,

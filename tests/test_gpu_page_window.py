@@ -128,6 +128,15 @@ def test_many_keys_in_the_line(dtype):
         assert not c.status.any()
 
 
+@pytest.mark.parametrize("ps", [32, 256, 1024])
+def test_other_page_sizes(ps):
+    for new, kv in (([1] * 4, [1100, 5, 2050, 700]), ([40, 130], [1500, 1030])):
+        for window, sinks in ((300, 17), (1030, 0)):
+            c = Case(ps + window, BF, 4, 2, 64, ps, new, kv, window, sinks)
+            c.check(c.run())
+            assert not c.status.any()
+
+
 def test_more_than_64_sequences():
     rng = np.random.default_rng(3)
     for n in (130, 70):

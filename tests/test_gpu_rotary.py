@@ -183,6 +183,17 @@ def test_pages(dtype, Hq, Hkv, d, ps):
         assert np.array_equal(to_host_bits(pages.k), want_k) and np.array_equal(to_host_bits(pages.v), want_v)
 
 
+def test_keys_and_values_alone():
+    x = Rows(15, BF, 40, 4, 2, 64)
+    slots = torch.arange(40, dtype=torch.int32, device="cuda")
+    one, two = A.Pages.empty(3, 2, 16, 64), A.Pages.empty(3, 2, 16, 64)
+    for p in (one, two):
+        p.k.zero_(), p.v.zero_()
+    A.prepare_page_store_rotary(one, Rotary(64), x.pos, None, None, x.k, x.v, slots, None, x.wk)()
+    A.page_store_rotary(two, Rotary(64), x.pos, x.q, x.k, x.v, slots, None, x.wk)
+    assert torch.equal(one.k, two.k) and torch.equal(one.v, two.v)
+
+
 def test_values_reach_the_pages_as_they_are():
     x = Rows(9, BF, 16, 2, 2, 64)
     bits = torch.arange(16 * 2 * 64, device="cuda", dtype=torch.int32).mul(37).to(torch.int16).view(16, 2, 64)

@@ -25,6 +25,14 @@ def test_turns_are_the_frequencies_fractions(rot, base):
             assert min(away, 2 ** 64 - away) <= Decimal(2)
 
 
+def test_turns_at_the_ends():
+    # a whole turn and a hair less are no turn; half a turn either way is the same
+    got = Rotary(16, [0.0, 2 * np.pi, -1e-300, np.pi, -np.pi, 1e-25, 0.0, 0.0], device="cpu").turns.numpy().view(np.uint64)
+    assert got[0] == got[2] == got[5] == 0
+    assert min(int(got[1]), 2 ** 64 - int(got[1])) < 2 ** 13       # (2 pi in 64 bits is off by 2.4e-16)
+    assert abs(int(got[3]) - 2 ** 63) < 2 ** 13 and abs(int(got[4]) - 2 ** 63) < 2 ** 13
+
+
 def test_frequencies():
     f, scale = rotary_frequencies(128, 1e4)
     assert scale == 1 and f[0] == 1 and np.isclose(f[63], 1e4 ** (-126 / 128))
