@@ -287,3 +287,31 @@ def test_graph():
         torch.cuda.synchronize()
         want = P.page_release(16, k, pool.lens, pool.table, pool.free, pool.count)
         assert np.array_equal(host(free), want[0]) and np.array_equal(host(out[0]), want[1]) and int(out[1]) == want[2]
+
+
+def test_other_streams():
+    pool, rng = families(12, 6, 5, 16, 700, 60)
+    B = 30
+    keep = np.where(rng.random(B) < 0.4, 0, pool.lens)
+    want = P.page_release(16, keep, pool.lens, pool.table, pool.free, pool.count)
+    parent, n = [-1] * B, [0] * B
+    lens = pool.lens.copy()
+    lens[[3, 9, 17]] = 0
+    for b in (3, 9, 17):
+        parent[b], n[b] = 5, int(lens[5])
+    wantf = P.page_fork(16, parent, n, lens, pool.free, pool.count, pool.table)
+    k = torch.randn(pool.n_pages, 2, 16, 64, device="cuda").bfloat16()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    free, table = ints(pool.free), ints(pool.table)
+    pages = A.Pages(k.clone(), k.clone())
+    args = ints(keep), ints(pool.lens), ints(pool.table), ints([pool.count]), ints(parent), ints(n), ints(lens), ints(pool.free)
+    torch.cuda.synchronize()
+    # both at once, each on its own state
+    got = A.page_release(16, args[0], args[1], args[2], free, args[3], stream=streams[0])
+    out = A.page_fork(16, args[4], args[5], args[6], args[7], args[3], table, stream=streams[1])
+    A.page_copy(pages, out[2], out[3], stream=streams[1])
+    torch.cuda.synchronize()
+    assert np.array_equal(host(free), want[0]) and np.array_equal(host(got[0]), want[1]) and int(got[1]) == want[2]
+    for g, w in zip((table, *out), (wantf[0], wantf[1], None, wantf[3], wantf[4])):
+        assert w is None or np.array_equal(host(g), w)
+    assert np.array_equal(to_host_bits(pages.v), P.page_copy(to_host_bits(k), wantf[3], wantf[4]))

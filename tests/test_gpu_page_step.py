@@ -255,3 +255,47 @@ def test_captured_step():
                 a, b = a[:int(caches[0].free_count)], b[:int(caches[0].free_count)]
             assert torch.equal(a, b), name
     assert int(caches[0].seq_len[0]) == 5 + 71 and int(caches[0].free_count) > 20
+
+
+def test_captured_forks():
+    # a graph that ends the questions and forks new ones off the same prompts
+    B, page = 6, 16
+    c = PagedCache(B, 60, 20, Hkv, d, page, layers=2, sharing=True)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    first = [75, 0, 0, 40, 0, 0]
+    rows = torch.randn(2, sum(first), 2 * Hkv, d, generator=gen, device="cuda").bfloat16()
+    c.reserve(ints(np.concatenate(([0], np.cumsum(first)))), sum(first))
+    for layer in range(2):
+        c.store(layer, rows[layer, :, :Hkv], rows[layer, :, Hkv:])
+    parent, keep = ints([-1, 0, 0, -1, 3, 0]), ints([75, 0, 0, 40, 0, 0])
+    status = torch.zeros(B, dtype=torch.int32, device="cuda")
+
+    def step():
+        c.trim(keep, status)
+        c.fork(parent, None, status)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    for i, p in enumerate(([-1, 0, 0, -1, 3, 0], [-1, 3, 3, -1, 0, -1], [-1, 0, -1, -1, 0, 3], [-1, -1, 3, -1, 3, 3])):
+        parent.copy_(ints(p))
+        g.replay()
+        torch.cuda.synchronize()
+        lens = [first[x] if x >= 0 else first[b] for b, x in enumerate(p)]
+        assert c.seq_len.tolist() == lens and not status.any()
+        held = {int(c.block_table[b, j]) for b in range(B) for j in range(-(-lens[b] // page))}
+        assert sorted(list(held) + c.free_pages[:int(c.free_count)].tolist()) == list(range(60))
+        for b, x in enumerate(p):
+            src = x if x >= 0 else b
+            at = torch.arange(lens[b], device="cuda")
+            pg = c.block_table[b, at // page].long()
+            r0 = 0 if src == 0 else 75
+            for layer in range(2):
+                got = c.layers[layer].k[pg, :, at % page]
+                assert torch.equal(got, rows[layer, r0:r0 + lens[b], :Hkv]), (i, b, layer)
