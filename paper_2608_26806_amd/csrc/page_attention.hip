@@ -1171,6 +1171,12 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
     L.brief = four > 0 || two > 0;
     if (L.half && two == 0.) L.brief = false;
   }
+  // Tiles of 32 rows: in one round only, and from 80 tiles on of more keys (over 3,000 keys,
+  // blocks that join / blocks of 128 rows: 300 tokens, window 64, 32/8 heads, 304 tiles 15.7
+  // / 12.4, 1,024, 28/4 heads, 264 tiles 32.4 / 23.6; 100 tokens, 1,024, 104 and 88 tiles
+  // 16.9 / 19.8 and 16.9 / 19.3; 30 tokens, 64 tiles 16.8 / 15.6).
+  if (alike && P.dtype == AVTP_BF16 && small == 32)
+    L.brief = now <= 256 * (P.d == 64 ? 2 : 1) && max_kv_len <= (now >= 80 ? kShortFullKeys : kShortKeys);
   // fp32 behind a window: where a block's waves (four, or two at d 128) have a few stages
   // each.  us, line or blocks of 128 rows against blocks that join, d 64 (14/2 heads) and
   // d 128 (16/8): 100 tokens, window 64 17.0 / 8.4 and 26.5 / 17.3, 256 18.9 / 14.2 and 27.6
