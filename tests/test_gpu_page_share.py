@@ -315,3 +315,31 @@ def test_other_streams():
     for g, w in zip((table, *out), (wantf[0], wantf[1], None, wantf[3], wantf[4])):
         assert w is None or np.array_equal(host(g), w)
     assert np.array_equal(to_host_bits(pages.v), P.page_copy(to_host_bits(k), wantf[3], wantf[4]))
+
+
+def test_as_many_sequences_as_there_may_be():
+    B, ps = 1 << 16, 16
+    rng = np.random.default_rng(13)
+    child = rng.random(B) < 0.5
+    child[0] = False
+    lens = np.where(child, 0, rng.integers(0, 40, B))
+    pool = Pool(13, lens, ps, 20000)
+    parent = np.where(child, rng.choice(np.nonzero(~child)[0], B), -1)
+    n = np.where(child, lens[np.maximum(parent, 0)], 0)
+    got = pool.fork(parent, n)
+    assert (got[6] & 32).any()                       # the stack does not last
+    pool.table, pool.lens, pool.count = got[0], got[1], got[2]
+    keep = np.where(rng.random(B) < 0.6, 0, pool.lens)
+    pool.release(keep)
+
+
+def test_pages_behind_four_gigabytes():
+    ps, Hkv, d = 64, 8, 128
+    n_pages = (5 << 30) // (ps * Hkv * d * 2)         # 5 GiB a tensor
+    pages = A.Pages.empty(n_pages, Hkv, ps, d)
+    last = n_pages - 1
+    x = torch.randn(2, Hkv, ps, d, device="cuda").bfloat16()
+    pages.k[last], pages.v[last] = x[0], x[1]
+    A.page_copy(pages, ints([last, last]), ints([3, last - 2]))
+    for p in (3, last - 2, last):
+        assert torch.equal(pages.k[p], x[0]) and torch.equal(pages.v[p], x[1])

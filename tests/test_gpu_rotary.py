@@ -204,6 +204,25 @@ def test_values_reach_the_pages_as_they_are():
     assert torch.equal(pages.v[0].transpose(0, 1).contiguous().view(torch.int16), bits)
 
 
+def test_slots_and_rows_behind_four_gigabytes():
+    ps, Hkv, d = 64, 8, 128
+    n_pages = (5 << 30) // (ps * Hkv * d * 2)
+    pages = A.Pages.empty(n_pages, Hkv, ps, d)
+    stride = 1 << 22                                  # 600 rows 8 MiB apart
+    base = torch.empty(600 * stride, dtype=BF, device="cuda")
+    rows = base.as_strided((600, 24, d), (stride, d, 1))
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    rows.copy_(torch.randn(600, 24, d, generator=gen, device="cuda"))
+    pos = torch.randint(0, 9999, (1, 600), generator=gen, device="cuda")
+    slots = torch.arange(n_pages * ps - 600, n_pages * ps, dtype=torch.int32, device="cuda")
+    rotary = Rotary(d, base=1e6)
+    got = A.page_store_rotary(pages, rotary, pos, rows[:, :8], rows[:, 8:16], rows[:, 16:], slots)
+    q, k = A.norm_rotary(rotary, pos, rows[:, :8].contiguous(), rows[:, 8:16].contiguous())
+    at = slots.long()
+    assert torch.equal(got, q) and torch.equal(pages.k[at // ps, :, at % ps], k)
+    assert torch.equal(pages.v[at // ps, :, at % ps], rows[:, 16:])
+
+
 def test_stream_and_graph():
     x = Rows(11, BF, 64, 8, 2, 128, 1)
     rotary = Rotary(128, base=1e6)
