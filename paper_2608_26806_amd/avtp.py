@@ -660,6 +660,10 @@ def _page_arg(t: Optional[torch.Tensor], name: str, numel: int = 0, dtype=torch.
     if t is not None and t.is_cuda and t.device.index != torch.cuda.current_device():
         raise ValueError(f"{name}: on {t.device}, the current device is "
                          f"cuda:{torch.cuda.current_device()}")
+    if numel < 0:  # (strided: the caller looks at the layout)
+        if not t.is_cuda:
+            raise ValueError(f"{name}: a GPU tensor is needed, got one on {t.device}")
+        return None
     return _arg(t, name, numel, dtype)
 
 
@@ -680,7 +684,7 @@ def _page_rows(t: torch.Tensor, name: str, heads: int, pages: "Pages"):
         raise ValueError(f"{name}: [N, {heads}, {pages.d}] is needed, got {tuple(t.shape)}")
     if t.dtype != pages.dtype:
         raise TypeError(f"{name}: {pages.dtype} is needed, got {t.dtype}")
-    _page_arg(t[:0].reshape(-1), name, 0, None)
+    _page_arg(t, name, -1)
     if t.shape[0] > 0 and (t.stride(2) != 1 or (heads > 1 and t.stride(1) != pages.d)):
         raise ValueError(f"{name}: the values of a token must be contiguous")
     stride = t.stride(0) if t.shape[0] > 1 else heads * pages.d
@@ -990,7 +994,7 @@ def _positions(rotary, pos: torch.Tensor, n: int):
         raise ValueError(f"pos: [{rotary.n_planes}, {n}] is needed, got {tuple(pos.shape)}")
     if p.dtype != torch.int64:
         raise TypeError(f"pos: {torch.int64} is needed, got {p.dtype}")
-    _page_arg(p[:0].reshape(-1), "pos", 0, None)
+    _page_arg(p, "pos", -1)
     if p.numel() and (p.shape[1] > 1 and p.stride(1) != 1):
         raise ValueError("pos: the positions of a plane must be contiguous")
     if p.shape[0] > 1 and p.stride(0) < n:

@@ -55,13 +55,13 @@ class PagedCache:
         self.sharing = sharing or window is not None
         self.layers = [A.Pages.empty(n_pages, Hkv, page_size, d, dtype, device) for _ in range(layers)]
         ints = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=device)  # noqa: E731
-        # lengths and the number of free pages side by side: one copy takes a
-        # call's results over
-        self._state, self._after = ints(requests + 1), ints(requests + 1)
-        self.seq_len, self.free_count = self._state[:requests], self._state[requests:]
+        # lengths, the number of free pages and (sharing) the tokens that have left each
+        # sequence's window side by side: one copy takes a call's results over
+        size = requests + 1 + (requests if self.sharing else 0)
+        self._state, self._after = ints(size), ints(size)
+        self.seq_len, self.free_count = self._state[:requests], self._state[requests:requests + 1]
         if self.sharing:
-            # tokens that have left each sequence's window, and scratch
-            self.gone, self._gone_after = ints(requests), ints(requests)
+            self.gone, self._gone_after = self._state[requests + 1:], self._after[requests + 1:]
             self._src, self._dst = ints(requests), ints(requests)
             self._ws = A.alloc_workspace(A.page_release_workspace_bytes(n_pages), device)
         # the lengths as attention takes them: 0 for requests whose last new tokens
@@ -130,7 +130,6 @@ class PagedCache:
             A.page_copy(pages, self._src, self._dst)
         # (attention takes a fork's tokens from its next reservation on)
         self._state.copy_(self._after)
-        self.gone.copy_(self._gone_after)
 
     def attend(self, layer: int, q: torch.Tensor, cu_q: torch.Tensor, softmax_scale: float,
                max_kv_len: Optional[int] = None, out: Optional[torch.Tensor] = None,
@@ -155,7 +154,6 @@ class PagedCache:
                                    self.sinks, self.gone, self._gone_after, status)()
             torch.minimum(self._seen, self._after[:B], out=self._seen)
             self._state.copy_(self._after)
-            self.gone.copy_(self._gone_after)
             return
         A.prepare_page_trim(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
                             self.free_count, self._after[:B], self._after[B:], status)()
