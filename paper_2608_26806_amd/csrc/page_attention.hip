@@ -1126,6 +1126,8 @@ constexpr int kManyWaves = 4;
 // length (60 of 10-2,000 keys, 28/4 heads, 19.8 -> 27.2).
 // fp32 keeps the line: 8 requests of 300 keys 16.6 -> 19.3.
 constexpr int kShortTiles = 384, kShortTiles64 = 512, kShortKeys = 1024, kShortFull = 128, kShortFullKeys = 2048;
+// single tokens behind a window (page_attn_plan)
+constexpr int kAlikeKeys = 2560;
 // 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
 constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
@@ -1156,9 +1158,10 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // tiles) 16.8 / 17.0 us, 16 22.9 / 19.0, 32 33.4 / 28.4, 48 44.3 / 39.5 (two waves;
   // four 46.7), 64 of which some are short 49.6 / 44.7, 80 65.8 / 62.2 (two 67.7), 96 76.2
   // / 69.1 (two 71.7), 128 97.5 / 87.8; window 256, 64 24.3 / 24.4 (four 34.5), 96 29.4 /
-  // 25.6 (four 30.9); window 3,000, 8 26.6 / 35.9, 40 86.6 / 88.4, 80 (two 0.63 full) 164 /
-  // 181, 96 194 / 182; 16/16 heads of 64, window 1,024, 8 (128 tiles) 17.5 / 14.1.
-  if (alike && !L.brief && P.dtype == AVTP_BF16 && small == 16) {
+  // 25.6 (four 30.9); 16/16 heads of 64, window 1,024, 8 (128 tiles) 17.5 / 14.1.  Longer
+  // windows are not worth it where lengths differ after all (64 requests of 300-20,000
+  // tokens, window 2,048 72.8 / 72.3, 4,096 111 / 115, 8,192 154 / 190; 16 4,096 36 / 48).
+  if (alike && !L.brief && max_kv_len <= kAlikeKeys && P.dtype == AVTP_BF16 && small == 16) {
     // the part of their places that the blocks of the last round and those before fill
     auto fill = [&](int waves) {
       const int64_t places = 1024 / waves * (P.d == 64 ? 2 : 1), rounds = (now + places - 1) / places;
@@ -1185,7 +1188,7 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // 11.3 / 9.0 and 15.2 / 18.5; 32 requests, 256 11.0 / 13.3 and (256 tiles) 32.1 / 27.2.
   if (w.window > 0 && P.dtype == AVTP_FP32) {
     const bool full = now >= kShortFull, narrow = P.d == 64;
-    const int64_t most = narrow && small == 32 ? (full ? kShortFullKeys : 512) : !narrow && small == 16 && full && alike ? seen : 128;
+    const int64_t most = narrow && small == 32 ? (full ? kShortFullKeys : 512) : !narrow && small == 16 && full && alike ? kAlikeKeys : 128;
     L.brief = now <= 256 ? max_kv_len <= most : narrow && small == 32 && now <= 512 && max_kv_len <= 260;
   }
   // Up to 32 rows a sequence is one tile of the even line; more rows read its keys once
