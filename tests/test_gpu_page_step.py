@@ -299,3 +299,50 @@ def test_captured_forks():
             for layer in range(2):
                 got = c.layers[layer].k[pg, :, at % page]
                 assert torch.equal(got, rows[layer, r0:r0 + lens[b], :Hkv]), (i, b, layer)
+
+
+@pytest.mark.parametrize("seed, window, sinks", [(1, None, 0), (2, None, 0), (3, 45, 4), (4, 1, 0), (5, 130, 40), (6, 30, 17)])
+def test_random_serving(seed, window, sinks):
+    # requests that come, grow, fork, are cut, refused and end, every step checked
+    rng = np.random.default_rng(seed)
+    B, page = 9, int(rng.choice([16, 32]))
+    s = Serving(seed, B, 170, page, sharing=True, window=window, sinks=sinks)
+    say(f"[page step] random serving, seed {seed}, window {window}, sinks {sinks}, page {page}")
+    refused = 0
+    for t in range(40):
+        L = np.array([len(k) for k in s.k[0]])
+        new = np.where(L == 0, np.where(rng.random(B) < 0.4, rng.integers(1, 90, B), 0),
+                       np.where(rng.random(B) < 0.8, rng.integers(1, 6, B), 0))
+        room = int(s.cache.free_count) * page - B * page
+        if L.max() + 100 < 64 * page and new.sum() < room:
+            s.step(new.tolist())
+        L = np.array([len(k) for k in s.k[0]])
+        keep = np.where(rng.random(B) < 0.12, 0, np.where(rng.random(B) < 0.3, np.maximum(L - rng.integers(0, 40, B), 0), L))
+        gone = s.cache.gone.tolist()
+        holds = {}
+        for b in range(B):
+            for j in range(-(-int(L[b]) // page)):
+                if j < -(-sinks // page) or j >= gone[b] // page:
+                    holds.setdefault(int(s.cache.block_table[b, j]), []).append(b)
+        flags = [0] * B
+        for b in range(B):
+            k = int(keep[b])
+            if 0 < k < L[b]:
+                shared = k % page and len(holds.get(int(s.cache.block_table[b, k // page]), [])) > 1
+                behind = gone[b] > 0 and k - (window or 0) + 1 < gone[b]
+                flags[b] = A.FLAG_REFUSED if shared or behind else 0
+        refused += sum(1 for f in flags if f)
+        s.cut(keep.tolist(), flags)
+        L = np.array([len(k) for k in s.k[0]])
+        empty, full = np.nonzero(L == 0)[0], np.nonzero(L > 0)[0]
+        if len(empty) and len(full) and int(s.cache.free_count) > B:
+            parent, n = np.full(B, -1), np.zeros(B, dtype=int)
+            for b in empty:
+                if rng.random() < 0.5:
+                    p = int(rng.choice(full))
+                    parent[b] = p
+                    n[b] = L[p] if int(s.cache.gone[p]) > 0 or rng.random() < 0.5 else rng.integers(0, L[p] + 1)
+            s.fork(parent.tolist(), n.tolist())
+    s.cut([0] * B)
+    assert int(s.cache.free_count) == 170
+    say(f"{refused} cuts refused")

@@ -294,3 +294,25 @@ def test_reruns_streams_and_graphs():
         eager = A.page_attention(c.pages, c.q, cu, kv, table, c.scale, 4000, window=1000, sinks=4)
         torch.cuda.synchronize()
         assert torch.equal(out, eager[0]) and torch.equal(lse, eager[1])
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_random_cases(seed):
+    rng = np.random.default_rng(1000 + seed)
+    dtype = BF if rng.random() < 0.7 else F
+    d = int(rng.choice([64, 128]))
+    Hkv = int(rng.choice([1, 2, 3]))
+    Hq = Hkv * int(rng.choice([1, 2, 4, 7, 9]))
+    B = int(rng.choice([1, 2, 5, 30, 70]))
+    kv = np.exp(rng.uniform(0, np.log(1500 if B < 10 else 250), B)).astype(int)
+    most = [1, 1, 4, 40, 150][rng.integers(5)] if B < 10 else [1, 1, 5, 20][rng.integers(4)]
+    new = np.minimum(rng.integers(0 if rng.random() < 0.3 else 1, most + 1, B), kv + rng.integers(0, 2, B))
+    if new.sum() == 0:
+        new[0] = 1
+    window = int(np.exp(rng.uniform(0, np.log(2000))))
+    sinks = int(rng.choice([0, 1, 4, 31, 32, 33, 64, 100, 300]))
+    c = Case(seed, dtype, Hq, Hkv, d, int(rng.choice([16, 32, 64, 256])), new.tolist(), kv.tolist(), window, sinks)
+    ref = c.oracle()
+    for bound in (int(kv.max()), int(rng.choice([1, 100, 4000, 100000]))):
+        c.check(c.run(max_kv=bound), ref)
+    assert not c.status.any()
