@@ -155,10 +155,15 @@ class PagedCache:
             torch.minimum(self._seen, self._after[:B], out=self._seen)
             self._state.copy_(self._after)
             return
+        self._cut(keep_len, status)
+
+    def _cut(self, keep_len: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
+        """Lengths and pages only, every page as its sequence's own."""
+        B = self.seq_len.numel()
         A.prepare_page_trim(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,
                             self.free_count, self._after[:B], self._after[B:], status)()
         torch.minimum(self._seen, self._after[:B], out=self._seen)
-        self._state.copy_(self._after)
+        self._state.copy_(self._after)  # (of a window what is there already)
 
     def _mark(self):
         """What ``_take_back`` needs to undo the reservations that follow."""
@@ -166,7 +171,10 @@ class PagedCache:
 
     def _take_back(self, mark) -> None:
         """Undo what was reserved since ``mark`` was made: the lengths are as they were
-        and the pages are free again (the ones taken last on top of the stack)."""
+        and the pages are free again (the ones taken last on top of the stack).  What has
+        left the windows stays as it is, so that tokens which wait for their attention
+        keep the keys they see; pages taken since are no other sequence's, so a cut
+        without a look at their holders is right for forks too."""
         seq_len, seen, self.slots = mark
-        self.trim(seq_len)
+        self._cut(seq_len)
         self._seen.copy_(seen)
