@@ -910,17 +910,20 @@ def prepare_page_fork(page_size: int, parent: torch.Tensor, fork_len: torch.Tens
 
 def page_fork(page_size: int, parent: torch.Tensor, fork_len: torch.Tensor, seq_len: torch.Tensor,
               free_pages: torch.Tensor, free_count: torch.Tensor, block_table: torch.Tensor,
-              status: Optional[torch.Tensor] = None, stream=None):
+              status: Optional[torch.Tensor] = None, stream=None, gone: Optional[torch.Tensor] = None):
     """Sequences that start from the first fork_len tokens of their parents
     (block_table is updated in place).  Returns (seq_len_out, free_count_out,
-    src_page, dst_page); ``page_copy`` takes the last two, in every layer."""
+    src_page, dst_page), and gone_out where gone is given; ``page_copy`` takes src_page
+    and dst_page, in every layer.  Once ``page_release`` has let go of tokens behind a
+    window its gone is needed here: a fork without it would count pages that have
+    left as its own, and a later release hand them back again."""
     new = lambda n: torch.empty(n, dtype=torch.int32, device=seq_len.device)  # noqa: E731
     B = seq_len.numel()
     with _on(stream, seq_len.device):
-        out = new(B), new(1), new(B), new(B)
+        out, gone_out = (new(B), new(1), new(B), new(B)), None if gone is None else new(B)
     prepare_page_fork(page_size, parent, fork_len, seq_len, free_pages, free_count, block_table, *out,
-                      status=status, stream=stream)()
-    return out
+                      gone=gone, gone_out=gone_out, status=status, stream=stream)()
+    return out if gone is None else (*out, gone_out)
 
 
 def prepare_page_copy(pages: Pages, src_page: torch.Tensor, dst_page: torch.Tensor, stream=None) -> Prepared:
