@@ -538,7 +538,8 @@ int avtp_page_attention_window(avtp_stream_t stream, const avtp_pages *pages, co
  *   gone, gone_out [B] (both or neither): avtp_page_release's; a fork has its parent's.
  *     They may be NULL only while no release has let go behind a window: a fork without
  *     them would hold pages that have left, and hand them back a second time.
- *   seq_len_out [B], free_count_out [1], src_page, dst_page [B] (outputs).
+ *   seq_len_out [B], free_count_out [1], src_page, dst_page [B] (outputs, which share no
+ *     memory with each other or with an input; so for avtp_page_release).
  * Pages are taken in the order of the sequences; one for which none is left stays as
  * it was and flags AVTP_FLAG_NO_PAGES (its later ones that need none are made).
  * Behind forks sequences are cut and ended with avtp_page_release: avtp_page_trim

@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "avtp_internal.h"
 
@@ -530,6 +531,26 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
                                       n_src, slot_map, keep_idx, n));
 }
 
+// elements of a call's buffer (p may be NULL)
+struct Ints {
+  const int32_t *p;
+  int64_t n;
+};
+static bool meet(const Ints &a, const Ints &b) {
+  const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+  return a.p && b.p && x < y + 4 * (uint64_t)b.n && y < x + 4 * (uint64_t)a.n;
+}
+// Does an output share memory with another one, or with what other blocks still read?
+static bool outputs_meet(std::initializer_list<Ints> outs, std::initializer_list<Ints> ins) {
+  for (const Ints *a = outs.begin(); a != outs.end(); ++a) {
+    for (const Ints *b = a + 1; b != outs.end(); ++b)
+      if (meet(*a, *b)) return true;
+    for (const Ints &b : ins)
+      if (meet(*a, b)) return true;
+  }
+  return false;
+}
+
 int avtp_page_fork(avtp_stream_t stream, int B, int page_size, const int32_t *parent,
                    const int32_t *fork_len, const int32_t *seq_len, const int32_t *free_pages,
                    int n_pages, const int32_t *free_count, int32_t *block_table, int max_pages,
@@ -540,10 +561,10 @@ int avtp_page_fork(avtp_stream_t stream, int B, int page_size, const int32_t *pa
   if (!parent || !fork_len || !seq_len || !free_pages || !free_count || !block_table || !seq_len_out ||
       !free_count_out || !src_page || !dst_page || !gone != !gone_out)
     return AVTP_ERR_INVALID_ARG;
-  // blocks read the state that another block would overwrite
-  for (const int32_t *out : {seq_len_out, src_page, dst_page, gone_out})
-    if (out && (out == parent || out == fork_len || out == seq_len || out == gone)) return AVTP_ERR_INVALID_ARG;
-  if (free_count_out == free_count) return AVTP_ERR_INVALID_ARG;
+  if (outputs_meet({{seq_len_out, B}, {free_count_out, 1}, {src_page, B}, {dst_page, B}, {gone_out, B}},
+                   {{parent, B}, {fork_len, B}, {seq_len, B}, {free_pages, n_pages}, {free_count, 1},
+                    {block_table, (int64_t)B * max_pages}, {gone, B}}))
+    return AVTP_ERR_INVALID_ARG;
   const PageFork F{B, __builtin_ctz((unsigned)page_size), max_pages, n_pages, parent, fork_len, seq_len, free_pages,
                    free_count, gone, block_table, seq_len_out, free_count_out, src_page, dst_page, gone_out, status};
   return hip_status(launch_page_fork((hipStream_t)stream, F));
@@ -576,11 +597,11 @@ int avtp_page_release(avtp_stream_t stream, int B, int page_size, const int32_t 
       window < 0 || sinks < 0 || !gone != !gone_out || (window > 0 && !gone))
     return AVTP_ERR_INVALID_ARG;
   if (window > 1 << 30 || sinks > 1 << 30) return AVTP_ERR_UNSUPPORTED;
-  // (waves of one row read what another would overwrite)
-  for (const int32_t *out : {seq_len_out, gone_out})
-    if (out && (out == keep_len || out == seq_len || out == gone)) return AVTP_ERR_INVALID_ARG;
-  if (seq_len_out == gone_out || free_count_out == free_count) return AVTP_ERR_INVALID_ARG;
   if (!ws || ws_bytes < page_release_workspace_bytes(n_pages) || (uintptr_t)ws % 256) return AVTP_ERR_WORKSPACE;
+  if (outputs_meet({{seq_len_out, B}, {free_count_out, 1}, {gone_out, B}},
+                   {{keep_len, B}, {seq_len, B}, {block_table, (int64_t)B * max_pages}, {free_pages, n_pages},
+                    {free_count, 1}, {gone, B}}))
+    return AVTP_ERR_INVALID_ARG;
   const PageRelease R{B, __builtin_ctz((unsigned)page_size), max_pages, n_pages, window, sinks, keep_len, seq_len,
                       block_table, free_count, gone, free_pages, seq_len_out, free_count_out, gone_out, status};
   return hip_status(launch_page_release((hipStream_t)stream, R, (int32_t *)ws));
