@@ -479,7 +479,8 @@ int avtp_page_store(avtp_stream_t stream, const avtp_pages *pages, const void *k
  * refer to a maximum that may lag behind, and then hold up to 2^13 for every token
  * a row sees: |v| may be 2^114 over the number of those tokens (2^97 of 131,072);
  * beyond it an output may overflow where the formula's quotient does not.  A row
- * whose logits are all -inf gives 0.
+ * whose logits are all -inf gives 0.  An infinite value whose weight is below 2^-126 of
+ * the row's largest gives infinity, as the formula does, or NaN (fp32's 0 times it).
  * ws: device scratch of avtp_page_attention_workspace_size() bytes (which may
  * be 0, and is for an invalid argument), 256-byte aligned, no initialisation;
  * it depends on the sizes alone, so that a call captured at the largest
