@@ -1128,6 +1128,8 @@ constexpr int kManyWaves = 4;
 constexpr int kShortTiles = 384, kShortTiles64 = 512, kShortKeys = 1024, kShortFull = 128, kShortFullKeys = 2048;
 // single tokens behind a window (page_attn_plan)
 constexpr int kAlikeKeys = 2560;
+// and chunks in fp32
+constexpr int kThreeStages = 320;
 // 32-key tiles of a stage: fp32 rows of 512 bytes fill a stage with one
 constexpr int many_tiles(int row_bytes) { return row_bytes > 256 ? 1 : 2; }
 
@@ -1186,10 +1188,15 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // / 32.6, 1,000 21.0 / 30.0; 300 tokens (131 tiles), 1,000 42.8 / 30.9; 1,000 tokens (440
   // tiles), 256 31.9 / 28.3, 1,000 57.8 / 60.1; one token, 64 11.0 / 5.5 and 15.0 / 10.4, 256
   // 11.3 / 9.0 and 15.2 / 18.5; 32 requests, 256 11.0 / 13.3 and (256 tiles) 32.1 / 27.2.
+  // Between 257 and 512 tiles of d 64 up to three stages a wave, which hold 320 keys beside the
+  // tile's own tokens and the ends of sinks and window (600 to 1,150 tokens and ten of 100, 14/2
+  // heads, blocks of 128 rows / blocks that join: 260 keys 25.7-31.5 / 26.7-29.4, 304 27.9-33.7 /
+  // 26.7-29.5, 344 27.5-38.0 / 29.2-34.2, 388 28.5-40.8 / 31.9-34.7; from there on now one, now
+  // the other).
   if (w.window > 0 && P.dtype == AVTP_FP32) {
     const bool full = now >= kShortFull, narrow = P.d == 64;
     const int64_t most = narrow && small == 32 ? (full ? kShortFullKeys : 512) : !narrow && small == 16 && full && alike ? kAlikeKeys : 128;
-    L.brief = now <= 256 ? max_kv_len <= most : narrow && small == 32 && now <= 512 && max_kv_len <= 260;
+    L.brief = now <= 256 ? max_kv_len <= most : narrow && small == 32 && now <= 512 && max_kv_len <= kThreeStages;
   }
   // Up to 32 rows a sequence is one tile of the even line; more rows read its keys once
   // per 32 there and once per 128 in a block.  us, line against blocks: 28/4 heads, 64

@@ -129,3 +129,12 @@ def test_single_tokens_that_see_everything(dtype, Hq, Hkv, d, sinks):
     ref = c.oracle()
     for bound in (513, 5000):
         c.check(c.run(max_kv=bound), ref)
+
+
+@pytest.mark.parametrize("window, sinks", [(256, 5), (316, 4), (317, 4)])
+def test_chunks_at_the_border_of_a_form(window, sinks):
+    # 440 tiles: blocks that join their waves' parts up to 320 keys, two launches behind
+    c = _case("steps", F, 14, 2, 64, [1000], [1700], window, sinks)
+    ws = A.page_attention_workspace_bytes(c.pages, 14, 1, c.q.shape[0], 1700, window, sinks)
+    assert (ws > 0) == (window + sinks > 320)
+    c.check(c.run(), _reference(c))
