@@ -542,7 +542,9 @@ int avtp_page_attention_window(avtp_stream_t stream, const avtp_pages *pages, co
  *   seq_len_out [B], free_count_out [1], src_page, dst_page [B] (outputs, which share no
  *     memory with each other or with an input; so for avtp_page_release).
  * Pages are taken in the order of the sequences; one for which none is left stays as
- * it was and flags AVTP_FLAG_NO_PAGES (its later ones that need none are made).
+ * it was and flags AVTP_FLAG_NO_PAGES (its later ones that need none are made).  Where
+ * the page to be copied, or the one off the stack, lies outside the pool the fork is made
+ * with nothing to copy and flags AVTP_FLAG_BAD_PAGE.
  * Behind forks sequences are cut and ended with avtp_page_release: avtp_page_trim
  * would hand a shared page back twice.
  *
@@ -555,10 +557,11 @@ int avtp_page_attention_window(avtp_stream_t stream, const avtp_pages *pages, co
  * pages whose tokens have left the window: gone_out[b] = keep - window + 1 (at least
  * gone[b]; 0 for one that has ended), and the pages of a row between those that hold
  * the first `sinks` tokens and page gone_out[b] / page_size are no longer its own,
- * whatever its entries say.  With no window gone may be NULL (nothing has left), or
- * is taken over.  A page goes onto the stack when no sequence holds it any more; the
- * pages freed by a call are pushed in ascending order.  Pages beyond the stack's
- * n_pages entries are dropped.
+ * whatever its entries say.  The next token's window starts at gone_out[b]: tokens that
+ * are stored and still wait for attention see further back, and come first.  With no
+ * window gone may be NULL (nothing has left), or is taken over.  A page goes onto the
+ * stack when no sequence holds it any more; the pages freed by a call are pushed in
+ * ascending order.  Pages beyond the stack's n_pages entries are dropped.
  *   A cut inside a page that another sequence held before the call would let it write
  *   into the other's tokens, and one to less than gone[b] + window - 1 tokens would
  *   leave tokens that have left the window missing: the sequence stays whole and flags

@@ -1163,6 +1163,8 @@ PageAttnPlan page_attn_plan(const avtp_pages &P, int Hq, int B, int64_t N_q, int
   // 25.6 (four 30.9); 16/16 heads of 64, window 1,024, 8 (128 tiles) 17.5 / 14.1.  Longer
   // windows are not worth it where lengths differ after all (64 requests of 300-20,000
   // tokens, window 2,048 72.8 / 72.3, 4,096 111 / 115, 8,192 154 / 190; 16 4,096 36 / 48).
+  // The line stays where two waves fill less and four lose: 80 requests, window 256 27.3, two
+  // 24.2, four 28.5.
   if (alike && !L.brief && max_kv_len <= kAlikeKeys && P.dtype == AVTP_BF16 && small == 16) {
     // the part of their places that the blocks of the last round and those before fill
     auto fill = [&](int waves) {

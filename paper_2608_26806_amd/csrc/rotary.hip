@@ -11,8 +11,9 @@
 // side: below 2^-28 behind the terms taken, about 2^-23 with their roundings.
 //
 // HBM-bound: every row is read once and written once.  133,120 rows of 32/8 heads of
-// 128 in bf16 (2.73 GB) take 465 us, 5.9 TB/s (a plain copy of 8 GB: 4.7); 64 rows of a
-// decode step 4.3 us, a launch and two dependent loads.
+// 128 take in bf16 465 us (2.73 GB, 5.9 TB/s; a plain copy of 4 GB 4.9), into pages with
+// their values 551 (3.27 GB, 5.9), in fp32 924 and 1,106; 64 rows of a decode step 4.3 us,
+// a launch and two dependent loads.
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -199,15 +200,15 @@ hipError_t launch(hipStream_t st, NArgs a) {
   constexpr int HPW = 64 / (D * (int)sizeof(T) / 32);
   const int most = (a.heads + HPW - 1) / HPW;
   // A wave for each 64 / TPH heads of few tokens; of tokens that fill the chip two or
-  // three times as many heads a wave, whose angles are computed less often (133,120 rows
-  // 463 us, 539 with one round of heads a wave, 477 with all five; 8,000 rows 37, 41
-  // and 42).
+  // three times as many heads a wave, whose angles are computed less often (both with
+  // cached stores: 133,120 rows 482 us, 540 with one round of heads a wave, 518 with all
+  // five; 8,000 rows 37, 41 and 42).
   constexpr long long kFull = 4096;
   a.groups = most / 2 > 1 ? most / 2 : 1;
   while (a.groups < most && a.r.n * a.groups < kFull) ++a.groups;
-  // Outputs of half of the Infinity Cache or more go past the caches: with a reader
-  // behind them 16,000 rows (164 MB written) take 115 us instead of 122, 8,000 rows 58.3
-  // instead of 57.6, 2,000 rows 17.1 instead of 16.0.
+  // Outputs of half of the Infinity Cache or more go past the caches (133,120 rows 482 ->
+  // 463 us): with a reader behind them 16,000 rows (164 MB written) take 115 us instead of
+  // 122, 8,000 rows 58.3 instead of 57.6, 2,000 rows 17.1 instead of 16.0.
   const bool stream = a.r.n * a.heads * D * (int)sizeof(T) >= 128ll << 20;
   const long long blocks = (a.r.n * a.groups + kWaves - 1) / kWaves;
   constexpr long long kWide = 1 << 20;  // blocks side by side (2^32 threads are too many for one axis)

@@ -19,14 +19,16 @@ and turns them in one call, and sequences may start from others' tokens:
     cache.fork(parent, fork_len)                       # more questions about the same images
 
 With a ``window`` (and ``sinks``) every ``attend`` sees the latest tokens and the
-first ones only, and ``trim`` also hands back the pages of what has left the window.
+first ones only, and ``trim`` also hands back the pages of what has left the window
+(so it comes behind the attention of the tokens reserved last, in every layer).
+A cache has one window: layers with another one, or with none, have a cache of their own.
 
 Every step runs in libavtp.so on torch's current stream (torch copies the new
 lengths over the old ones); nothing is read back to the host, and the state
 lies in buffers that stay where they are, so the calls of a decode step can be
 captured into a graph and replayed.  ``seq_len``, ``free_count``,
-``block_table`` and ``free_pages`` are there to be read; ``reserve`` and
-``trim`` change them.
+``block_table`` and ``free_pages`` are there to be read; ``reserve``, ``fork``
+and ``trim`` change them.
 """
 from __future__ import annotations
 
@@ -117,7 +119,8 @@ class PagedCache:
         """Every empty sequence b with parent[b] >= 0 gets the first fork_len[b] tokens
         of that sequence (all of them without a fork_len): their whole pages are shared, a
         last one filled in part is copied in every layer.  One that cannot be forked stays
-        empty and flags FLAG_REFUSED, or FLAG_NO_PAGES, in ``status`` [B]."""
+        empty and flags FLAG_REFUSED, or FLAG_NO_PAGES, in ``status`` [B].  ``attend`` takes
+        a fork's tokens from its next reservation on."""
         if not self.sharing:
             raise ValueError("a cache made with sharing=True is needed")
         B = self.seq_len.numel()
@@ -128,7 +131,6 @@ class PagedCache:
                             self.gone, self._gone_after, status)()
         for pages in self.layers:
             A.page_copy(pages, self._src, self._dst)
-        # (attention takes a fork's tokens from its next reservation on)
         self._state.copy_(self._after)
 
     def attend(self, layer: int, q: torch.Tensor, cu_q: torch.Tensor, softmax_scale: float,
@@ -144,9 +146,11 @@ class PagedCache:
 
     def trim(self, keep_len: torch.Tensor, status: Optional[torch.Tensor] = None) -> None:
         """Cut every sequence to its first keep_len tokens (0: it has ended), and with a
-        window let go of what has left it.  With sharing, a cut inside a page that
-        another sequence holds, or behind what the window has left, is refused: the
-        sequence stays whole and flags FLAG_REFUSED in ``status`` [B]."""
+        window let go of what has left it, as the next token sees it: tokens that were
+        reserved and still wait for ``attend`` see further back and come first.  With
+        sharing, a cut inside a page that another sequence holds, or behind what the
+        window has left, is refused: the sequence stays whole and flags FLAG_REFUSED in
+        ``status`` [B]."""
         B = self.seq_len.numel()
         if self.sharing:
             A.prepare_page_release(self.page_size, keep_len, self.seq_len, self.block_table, self.free_pages,

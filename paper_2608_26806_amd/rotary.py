@@ -29,14 +29,18 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, stretch: Optional[st
     """Frequencies (radians a position, float64 [rot_dim / 2]) and the scale of
     the rotated values: base^(-2 i / rot_dim), and by ``stretch``
 
-    - ``"linear"``: all divided by ``factor`` (positions drawn together);
+    - ``"linear"``: all divided by ``factor`` (positions drawn together; position
+      interpolation, arXiv:2306.15595);
     - ``"base"``: from base * factor^(rot_dim / (rot_dim - 2)), so that the slowest
-      pair is divided by ``factor`` and the fastest stays;
+      pair is divided by ``factor`` and the fastest stays ("NTK-aware", described in
+      arXiv:2309.00071);
     - ``"parts"``: pairs that make ``fast`` turns or more within ``trained``
       positions stay, those that make ``slow`` or fewer are divided by
-      ``factor``, linearly in the pair's number between; values scaled by
-      0.1 ln(factor) + 1;
-    - ``"wavelength"``: the same borders, linearly in the number of turns, not scaled.
+      ``factor``, linearly in the pair's number between (the borders moved outwards to
+      whole pairs, the first of which always stays); values scaled by 0.1 ln(factor) + 1
+      (YaRN, arXiv:2309.00071, its ramp taken over the pairs);
+    - ``"wavelength"``: the same borders, linearly in the number of turns, not scaled
+      ("NTK-by-parts" of the same paper).
     """
     if rot_dim < 4 or rot_dim % 2 or not base > 0 or not factor >= 1:
         raise ValueError("an even rot_dim of 4 or more, a positive base and a factor of 1 or more are needed")
@@ -57,7 +61,7 @@ def rotary_frequencies(rot_dim: int, base: float = 10000.0, stretch: Optional[st
         return f * stay + f / factor * (1 - stay), 1.0
     pair = lambda turns: rot_dim * math.log(trained / (2 * math.pi * turns)) / (2 * math.log(base))  # noqa: E731
     first, last = max(0, math.floor(pair(fast))), min(rot_dim - 1, math.ceil(pair(slow)))
-    stay = 1 - np.clip((i - first) / max(last - first, 0.001), 0, 1)
+    stay = 1 - np.clip((i - first) / max(last - first, 0.001), 0, 1)  # (both borders on one pair: a step)
     return f * stay + f / factor * (1 - stay), 0.1 * math.log(factor) + 1
 
 
